@@ -1,0 +1,461 @@
+"""What the operators of a quantised model's layers and of its answers are measured on.
+
+A case is a dict of plain values; its "op" says which operator a pass is:
+
+  few             a linear layer for a few tokens (generation): y = act(x W^T + bias) * mul + residual, W as 4-bit codes,
+                  block constants and an outlier list; every weight is m * level, a listed one its stored value
+  many            the same for many tokens (a batch, a prompt, a training step), over the decoder's bfloat16 weights; may
+                  also keep the pre-activation
+  grad            the gradients of `many`: by x, by the factor mul, by the bias
+  logprobs        log probabilities of given tokens from logits, the entropy of every row, the largest alternatives
+  logprobs_grad   the gradient of those log probabilities and entropies by the logits
+
+With `own` false `run` computes them from elementary torch operations in binary32, from the same codes, constants, lists,
+activations and logits; with `own` true it calls paper_2505_06653_amd.binding.
+"""
+import math
+from statistics import NormalDist
+
+import torch
+
+own = False
+
+# Levels of a signed-absmax codebook for blocks of 64 (0 and +1 are pinned; -1 is not a level).
+LEVELS = (-0.8568463921546936, -0.6692874431610107, -0.5235266089439392, -0.4004882574081421, -0.2910638153553009,
+          -0.1900092959403992, -0.0938529595732689, 0.0, 0.0887671709060669, 0.1794802695512772, 0.2743096053600311,
+          0.3760197460651398, 0.4886530041694641, 0.6188603639602661, 0.7791395783424377, 1.0)
+DEV = "cuda"
+DTYPE = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def listed():
+    return [
+        # Generation with a small odd-sized projection, three sequences at once: the call's latency.
+        {"name": "few_small_3tok", "op": "few", "rows": 1001, "cols": 1504, "block": 32, "opq": 0, "tokens": 3,
+         "act": "gelu_tanh", "bias": 1, "mul": 0, "residual": 1, "out": "bf16"},
+        # Generation, one sequence, the last matrix of a Llama-7B-shaped block: its result joins the residual stream.
+        {"name": "few_7b_down_opq", "op": "few", "rows": 4096, "cols": 11008, "block": 64, "opq": 1, "tokens": 1,
+         "act": "none", "bias": 0, "mul": 0, "residual": 1, "out": "bf16"},
+        # A batch of sequences in generation through the q, k, v projections with their bias.
+        {"name": "many_7b_qkv_24tok", "op": "many", "rows": 12288, "cols": 4096, "block": 64, "opq": 0, "tokens": 24,
+         "act": "none", "bias": 1, "mul": 0, "residual": 0, "pre": 0, "out": "bf16"},
+        # A training step's forward pass through the gate projection: gated by the up projection's result, the
+        # pre-activation kept; outliers apart.
+        {"name": "many_7b_gate_500tok_opq", "op": "many", "rows": 11008, "cols": 4096, "block": 64, "opq": 1,
+         "tokens": 500, "act": "silu", "bias": 0, "mul": 1, "residual": 0, "pre": 1, "out": "bf16"},
+        # A prompt of 2000 tokens through the last matrix of a block, into a residual stream in binary32.
+        {"name": "many_7b_down_2000tok", "op": "many", "rows": 4096, "cols": 11008, "block": 128, "opq": 0,
+         "tokens": 2000, "act": "none", "bias": 0, "mul": 0, "residual": 1, "pre": 0, "out": "f32"},
+        # Back through a square projection with an activation and a trained bias, an odd number of tokens.
+        {"name": "grad_square_333tok", "op": "grad", "rows": 4096, "cols": 4096, "block": 64, "opq": 0, "tokens": 333,
+         "act": "gelu", "bias": 1, "mul": 0, "out": "bf16"},
+        # Back through the gate projection of a training step of 2000 tokens, outliers apart.
+        {"name": "grad_7b_gate_2000tok_opq", "op": "grad", "rows": 11008, "cols": 4096, "block": 64, "opq": 1,
+         "tokens": 2000, "act": "silu", "bias": 0, "mul": 1, "out": "bf16"},
+        # Generation: what three sequences answer next, with twenty alternatives, from a vocabulary of 128000.
+        {"name": "logprobs_3rows_top20", "op": "logprobs", "rows": 3, "vocab": 128000, "logits": "f32", "top": 20,
+         "masked": 0},
+        # A batch with an odd vocabulary in bfloat16, a third of it ruled out, five alternatives.
+        {"name": "logprobs_100rows_bf16_masked", "op": "logprobs", "rows": 100, "vocab": 50257, "logits": "bf16", "top": 5,
+         "masked": 1},
+        # Scoring a text of 2000 tokens (perplexity), with the most likely token of every position.
+        {"name": "logprobs_2000rows", "op": "logprobs", "rows": 2000, "vocab": 32000, "logits": "f32", "top": 1,
+         "masked": 0},
+        # A training step's loss of 2000 tokens with an entropy term, back to the logits.
+        {"name": "logprobs_grad_2000rows", "op": "logprobs_grad", "rows": 2000, "vocab": 32000, "logits": "f32",
+         "entropy": 1, "masked": 0, "out": "bf16"},
+        # A few rows of an odd vocabulary in bfloat16 under a mask, log probabilities alone.
+        {"name": "logprobs_grad_30rows_bf16", "op": "logprobs_grad", "rows": 30, "vocab": 50257, "logits": "bf16",
+         "entropy": 0, "masked": 1, "out": "bf16"},
+    ]
+
+
+def _log_uniform(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(["few", "few", "many", "many", "grad", "grad", "logprobs", "logprobs", "logprobs_grad"])
+    if op in ("few", "many", "grad"):
+        block = rng.choice([32, 64, 64, 128, 256])
+        rows = _log_uniform(rng, 300, 28672)
+        cols = max(1, _log_uniform(rng, 512, 28672) // block) * block
+        rows = min(rows, 8192 * 28672 // cols)
+        tokens = rng.choice([1, 1, 2, 3, 4, 6]) if op == "few" else _log_uniform(rng, 5, 2500)
+        while rows * cols * tokens > 4096 * 11008 * 2000:
+            tokens //= 2
+        case = {"op": op, "rows": rows, "cols": cols, "block": block, "opq": rng.choice([0, 1]), "tokens": max(1, tokens),
+                "act": rng.choice(["none", "none", "relu", "gelu", "gelu_tanh", "silu"]), "bias": rng.choice([0, 1]),
+                "mul": rng.choice([0, 1]), "out": "bf16"}
+        if op != "grad":
+            case.update(residual=rng.choice([0, 1]), out=rng.choice(["bf16", "bf16", "f32"]))
+        if op == "many":
+            case["pre"] = rng.choice([0, 1])
+        return case
+    vocab = _log_uniform(rng, 500, 200000)
+    rows = min(_log_uniform(rng, 1, 4096), 2000 * 32000 // vocab)
+    case = {"op": op, "rows": rows, "vocab": vocab, "logits": rng.choice(["f32", "bf16"]), "masked": rng.choice([0, 0, 1])}
+    if op == "logprobs":
+        case["top"] = rng.choice([0, 1, 5, 20, 32])
+    else:
+        case.update(entropy=rng.choice([0, 1]), out=rng.choice(["bf16", "f32"]))
+    return case
+
+
+# ------------------------------------------------------------------------------------------------ inputs
+def _weights(rows, cols, g):
+    """Heavy-tailed weights (Student t with five degrees of freedom) with a scale for every row, in bfloat16."""
+    w = torch.randn((rows, cols), generator=g, device=DEV)
+    d = torch.zeros_like(w)
+    for _ in range(5):
+        d += torch.randn((rows, cols), generator=g, device=DEV).square_()
+    scale = 0.02 * torch.exp(0.3 * torch.randn((rows, 1), generator=g, device=DEV))
+    return (w * torch.rsqrt(d / 5) * scale).to(torch.bfloat16)
+
+
+def _quantize(w, block, opq):
+    """Codes (two to a byte, the first in the low nibble), binary16 block constants (signed maxima), outlier list."""
+    b = w.float().reshape(-1, block)
+    idx = val = None
+    if opq:  # what lies beyond the 0.95 quantile of the maximum of `block` normal numbers of the block's deviation
+        far = b.abs() > NormalDist().inv_cdf((1 + 0.95 ** (1 / block)) / 2) * b.std(1, keepdim=True)
+        idx = far.reshape(-1).nonzero().reshape(-1)
+        val = b.reshape(-1)[idx].to(torch.float16)
+        b = torch.where(far, 0.0, b)
+    at = b.abs().argmax(1, keepdim=True)
+    m = b.gather(1, at).to(torch.float16)
+    x = torch.nan_to_num(b / m.float())
+    lv = torch.tensor(LEVELS, dtype=torch.float32, device=DEV)
+    codes = torch.bucketize(x, (lv[1:] + lv[:-1]) / 2).to(torch.uint8).reshape(-1)
+    return (codes[0::2] | (codes[1::2] << 4)).contiguous(), m.reshape(-1).contiguous(), idx, val
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1000 * seed + 17)
+    st = {"case": case}
+    if case["op"] in ("logprobs", "logprobs_grad"):
+        return _prepare_logits(case, g, st)
+    rows, cols, block, t = case["rows"], case["cols"], case["block"], case["tokens"]
+    st["codes"], st["scales"], st["idx"], st["val"] = _quantize(_weights(rows, cols, g), block, case["opq"])
+
+    def activations(n, scale=1.0):
+        return (scale * torch.randn((t, n), generator=g, device=DEV)).to(torch.bfloat16)
+
+    st["bias"] = (0.1 * torch.randn(rows, generator=g, device=DEV)).to(torch.bfloat16) if case["bias"] else None
+    st["mul"] = activations(rows) if case["mul"] else None
+    if case["op"] == "grad":
+        st["dy"] = activations(rows, 0.01)
+        st["pre"] = activations(rows)
+    else:
+        st["x"] = activations(cols)
+        st["residual"] = (2.0 * torch.randn((t, rows), generator=g, device=DEV)).to(DTYPE[case["out"]]) if case["residual"] else None
+    if own:
+        _plan(case, st)
+    return st
+
+
+def _plan(case, st):
+    """What a program that uses the framework keeps next to the quantised matrix: the copy and the table that the products
+    read, workspaces, results' buffers."""
+    import numpy as np
+
+    from paper_2505_06653_amd import binding
+
+    rows, cols, block, t = case["rows"], case["cols"], case["block"], case["tokens"]
+    st["binding"], st["cb"] = binding, np.array(LEVELS, dtype=np.float64)
+    k = st["k"] = 0 if st["idx"] is None else int(st["idx"].numel())
+    make = binding.bof4_gemv_outlier_table if case["op"] == "few" else binding.bof4_gemm_outlier_table
+    st["table"] = make(st["codes"], st["scales"], rows, cols, block, st["cb"], st["idx"], st["val"]) if k else None
+    st["y"] = torch.empty((t, cols if case["op"] == "grad" else rows), dtype=DTYPE[case["out"]], device=DEV)
+    if case["op"] == "few":
+        return
+    st["packed"] = binding.bof4_gemm_pack(st["codes"], st["scales"], rows, cols, block)
+    if case["op"] == "many":
+        st["pre"] = torch.empty((t, rows), dtype=torch.bfloat16, device=DEV) if case["pre"] else None
+        size = binding.bof4_gemm_linear_workspace_bytes(rows, cols, t)
+    else:
+        st["dmul"] = torch.empty((t, rows), dtype=torch.bfloat16, device=DEV) if case["mul"] else None
+        st["dbias"] = torch.empty(rows, dtype=torch.float32, device=DEV) if case["bias"] else None
+        size = binding.bof4_gemm_linear_backward_workspace_bytes(rows, cols, t)
+    st["ws"] = torch.empty(size, dtype=torch.uint8, device=DEV)
+
+
+def _prepare_logits(case, g, st):
+    """Logits of a language model: a broad normal part and a few likely tokens in every row; one row in twenty asks for
+    no token (a padded place of a batch)."""
+    n, v = case["rows"], case["vocab"]
+    x = 2.5 * torch.randn((n, v), generator=g, device=DEV)
+    likely = torch.randint(0, v, (n, 4), generator=g, device=DEV)
+    x.scatter_add_(1, likely, 4.0 + 10.0 * torch.rand((n, 4), generator=g, device=DEV))
+    target = torch.where(torch.rand(n, generator=g, device=DEV) < 0.6, likely[:, 0],
+                         torch.randint(0, v, (n,), generator=g, device=DEV))
+    if case["masked"]:  # tokens that may not come next
+        out = torch.rand(v, generator=g, device=DEV) < 0.33
+        x.masked_fill_(out, -math.inf)
+        x.scatter_(1, target[:, None], 3.0)
+    st["target"] = torch.where(torch.rand(n, generator=g, device=DEV) < 0.05, -100, target)
+    st["logits"] = x.to(DTYPE[case["logits"]])
+    if own:
+        from paper_2505_06653_amd import binding
+
+        st["binding"] = binding
+    if case["op"] == "logprobs":
+        if own:
+            st["ws"] = torch.empty(binding.bof4_token_logprobs_workspace_bytes(n, v, case["top"]), dtype=torch.uint8, device=DEV)
+        return st
+    st["d_logprob"] = torch.where(st["target"] >= 0, -1.0 / n, 0.0).to(torch.float32)
+    st["d_entropy"] = 0.01 / n * torch.rand(n, generator=g, device=DEV) if case["entropy"] else None
+    if own:
+        _, st["entropy"], _, _, st["stats"] = binding.bof4_token_logprobs(st["logits"], st["target"])
+        st["out"] = torch.empty((n, v), dtype=DTYPE[case["out"]], device=DEV)
+    else:
+        logp, p, st["entropy"] = _distribution(st["logits"])
+        st["lse"] = _lse(st["logits"].float())
+        del logp, p
+    return st
+
+
+# ------------------------------------------------------------------------------------------------ one pass
+def run(st):
+    case = st["case"]
+    if own:
+        return _run_own(case, st)
+    if case["op"] == "logprobs":
+        return _plain_logprobs(case, st)
+    if case["op"] == "logprobs_grad":
+        return _plain_logprobs_grad(case, st)
+    w = _plain_weights(case, st)
+    if case["op"] == "grad":
+        z, dy = st["pre"].float(), st["dy"].float()
+        dz = dy * _plain_act_slope(case["act"], z)
+        if st["mul"] is not None:
+            dz = dz * st["mul"].float()
+        got = [(dz @ w).to(DTYPE[case["out"]])]
+        if st["mul"] is not None:
+            got.append((dy * _plain_act(case["act"], z)).to(torch.bfloat16))
+        if st["bias"] is not None:
+            got.append(dz.sum(0))
+        return got
+    z = st["x"].float() @ w.t()
+    if st["bias"] is not None:
+        z = z + st["bias"].float()
+    y = _plain_act(case["act"], z)
+    if st["mul"] is not None:
+        y = y * st["mul"].float()
+    if st["residual"] is not None:
+        y = y + st["residual"].float()
+    got = [y.to(DTYPE[case["out"]])]
+    if case.get("pre"):
+        got.append(z.to(torch.bfloat16))
+    return got
+
+
+def _run_own(case, st):
+    b, op = st["binding"], case["op"]
+    if op == "logprobs":
+        logprob, entropy, ids, top, _ = b.bof4_token_logprobs(st["logits"], st["target"], top=case["top"], ws=st["ws"])
+        return [logprob, entropy, ids, top] if case["top"] else [logprob, entropy]
+    if op == "logprobs_grad":
+        return [b.bof4_token_logprobs_backward(st["logits"], st["stats"], st["target"], st["d_logprob"], st["entropy"],
+                                               st["d_entropy"], out=st["out"])]
+    rows, cols = case["rows"], case["cols"]
+    if op == "few":
+        return [b.bof4_gemv_linear(st["codes"], st["scales"], rows, cols, case["block"], st["cb"], st["x"], st["table"],
+                                   st["k"], bias=st["bias"], act=case["act"], mul=st["mul"], residual=st["residual"],
+                                   out=st["y"])]
+    if op == "many":
+        y = b.bof4_gemm_linear(st["packed"], rows, cols, st["cb"], st["x"], st["table"], st["k"], bias=st["bias"],
+                               act=case["act"], mul=st["mul"], residual=st["residual"], pre=st["pre"], out=st["y"],
+                               ws=st["ws"])
+        return [y, st["pre"]] if case["pre"] else [y]
+    dx = b.bof4_gemm_linear_backward(st["packed"], rows, cols, st["cb"], st["dy"], st["table"], st["k"], act=case["act"],
+                                     pre=st["pre"], mul=st["mul"], dmul=st["dmul"], dbias=st["dbias"], out=st["y"],
+                                     ws=st["ws"])
+    return [dx] + [v for v in (st["dmul"], st["dbias"]) if v is not None]
+
+
+# ------------------------------------------------------------------------------------------------ the plain forms
+def _plain_weights(case, st):
+    """The matrix in binary32: m * level, listed positions as stored; for many tokens rounded to bfloat16, as the decoder
+    writes it."""
+    lv = torch.tensor(LEVELS, dtype=torch.float32, device=DEV)
+    codes = torch.stack((st["codes"] & 15, st["codes"] >> 4), 1).reshape(-1, case["block"])
+    w = (lv[codes.int()] * st["scales"].float()[:, None]).reshape(-1)
+    if st["idx"] is not None:
+        w[st["idx"]] = st["val"].float()
+    if case["op"] != "few":
+        w = w.to(torch.bfloat16).float()
+    return w.reshape(case["rows"], case["cols"])
+
+
+def _plain_act(act, z):
+    if act == "relu":
+        return torch.where(z > 0, z, 0.0)
+    if act == "gelu":
+        return 0.5 * z * (1 + torch.erf(z * math.sqrt(0.5)))
+    if act == "gelu_tanh":
+        return 0.5 * z * (1 + torch.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z * z * z)))
+    if act == "silu":
+        return z / (1 + torch.exp(-z))
+    return z
+
+
+def _plain_act_slope(act, z):
+    if act == "relu":
+        return torch.where(z > 0, 1.0, 0.0)
+    if act == "gelu":
+        return 0.5 * (1 + torch.erf(z * math.sqrt(0.5))) + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+    if act == "gelu_tanh":
+        a = math.sqrt(2 / math.pi)
+        t = torch.tanh(a * (z + 0.044715 * z * z * z))
+        return 0.5 * (1 + t) + 0.5 * z * (1 - t * t) * a * (1 + 3 * 0.044715 * z * z)
+    if act == "silu":
+        s = 1 / (1 + torch.exp(-z))
+        return s * (1 + z * (1 - s))
+    return torch.ones_like(z)
+
+
+def _lse(x):
+    m = x.max(1, keepdim=True).values
+    return m + torch.log(torch.exp(x - m).sum(1, keepdim=True))
+
+
+def _distribution(logits):
+    """log p, p and the entropy of every row, in binary32."""
+    x = logits.float()
+    logp = x - _lse(x)
+    p = torch.exp(logp)
+    entropy = -torch.where(p > 0, p * logp, 0.0).sum(1)
+    return logp, p, entropy
+
+
+def _plain_logprobs(case, st):
+    logp, _, entropy = _distribution(st["logits"])
+    target = st["target"]
+    lp = torch.where(target >= 0, logp.gather(1, target.clamp(min=0)[:, None])[:, 0], 0.0)
+    if not case["top"]:
+        return [lp, entropy]
+    # the largest logits, the lowest id first among equals: one whole number that orders both
+    x = st["logits"].float()
+    bits = x.view(torch.int32).long()
+    bits = torch.where(bits < 0, -(bits & 0x7FFFFFFF), bits)
+    key = bits * (1 << 20) - torch.arange(case["vocab"], device=DEV)
+    ids = key.topk(case["top"], 1, sorted=True).indices
+    return [lp, entropy, ids, logp.gather(1, ids)]
+
+
+def _plain_logprobs_grad(case, st):
+    logp = st["logits"].float() - st["lse"]
+    p = torch.exp(logp)
+    g = -st["d_logprob"][:, None] * p
+    target = st["target"]
+    g.scatter_add_(1, target.clamp(min=0)[:, None], torch.where(target >= 0, st["d_logprob"], 0.0)[:, None])
+    if st["d_entropy"] is not None:
+        g = g - st["d_entropy"][:, None] * torch.where(p > 0, p * (logp + st["entropy"][:, None]), 0.0)
+    return [g.to(DTYPE[case["out"]])]
+
+
+# ------------------------------------------------------------------------------------------------ the work of a pass
+_LISTED = 0.0066  # share of Student-t weights that the outlier rule lists
+
+
+def work(case):
+    if case["op"] in ("logprobs", "logprobs_grad"):
+        n = case["rows"] * case["vocab"]
+        size = {"bf16": 2, "f32": 4}
+        if case["op"] == "logprobs":
+            return {"bytes": n * size[case["logits"]] + case["rows"] * (16 + 12 * case["top"]), "flops": 6.0 * n}
+        return {"bytes": n * (size[case["logits"]] + size[case["out"]]) + 24 * case["rows"], "flops": 8.0 * n}
+    rows, cols, t = case["rows"], case["cols"], case["tokens"]
+    bytes_ = rows * cols * (0.5 + 2.0 / case["block"])
+    if case["opq"]:
+        bytes_ += _LISTED * rows * cols * (8 if case["op"] == "few" else 4)
+    out = {"bf16": 2, "f32": 4}[case["out"]]
+    if case["op"] == "grad":
+        bytes_ += t * cols * out + t * rows * (4 + 4 * case["mul"]) + 4 * rows * case["bias"]
+    else:
+        bytes_ += t * cols * 2 + t * rows * (out * (1 + case["residual"]) + 2 * case["mul"] + 2 * case.get("pre", 0)) + 2 * rows * case["bias"]
+    return {"bytes": float(bytes_), "flops": 2.0 * rows * cols * t}
+
+
+# ------------------------------------------------------------------------------------------------ from the definitions, in 64 bits
+def exact(case, seed):
+    global own
+    kept, own = own, False
+    try:
+        st = prepare(case, seed)
+    finally:
+        own = kept
+    f = torch.float64
+    if case["op"] in ("logprobs", "logprobs_grad"):
+        x = st["logits"].to(f)
+        rest = x - x.amax(1, keepdim=True)
+        logp = rest - rest.exp().sum(1, keepdim=True).log()
+        p = logp.exp()
+        h = -(p * logp.clamp(min=-1e300)).sum(1)
+        t = st["target"]
+        has = t >= 0
+        if case["op"] == "logprobs":
+            lp = torch.zeros(case["rows"], dtype=f, device=DEV)
+            lp[has] = logp[has, t[has]]
+            if not case["top"]:
+                return [lp, h]
+            ids = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :case["top"]].contiguous()
+            return [lp, h, ids, logp.gather(1, ids)]
+        g = st["d_logprob"].to(f)[:, None] * -p
+        g[has, t[has]] += st["d_logprob"].to(f)[has]
+        if st["d_entropy"] is not None:
+            g -= st["d_entropy"].to(f)[:, None] * p * (logp.clamp(min=-1e300) + h[:, None])
+        return [g]
+    rows, cols = case["rows"], case["cols"]
+    # both weights of a byte from a table of the 256 bytes
+    lv = torch.tensor(LEVELS, dtype=torch.float32, device=DEV)
+    byte = torch.arange(256, device=DEV)
+    pair = torch.stack((lv[byte % 16], lv[byte // 16]), 1)
+    level = pair[st["codes"].long()].reshape(-1, case["block"])
+    m = st["scales"].reshape(-1, 1)
+    if case["op"] == "few":
+        w = (level.to(f) * m.to(f)).reshape(-1)
+        listed_values = None if st["val"] is None else st["val"].to(f)
+    else:  # (the decoder's weights are defined by these two roundings)
+        w = (level * m.float()).to(torch.bfloat16).to(f).reshape(-1)
+        listed_values = None if st["val"] is None else st["val"].to(torch.bfloat16).to(f)
+    if listed_values is not None:
+        w.index_copy_(0, st["idx"], listed_values)
+    w = w.reshape(rows, cols)
+    if case["op"] == "grad":
+        z = st["pre"].to(f)
+        a, slope = _exact_act(case["act"], z)
+        dz = st["dy"].to(f) * slope
+        got = []
+        if st["mul"] is not None:
+            dz = dz * st["mul"].to(f)
+            got.append(st["dy"].to(f) * a)
+        if st["bias"] is not None:
+            got.append(dz.sum(0))
+        return [torch.mm(dz, w)] + got
+    z = torch.mm(w, st["x"].to(f).t().contiguous()).t()
+    if st["bias"] is not None:
+        z = z + st["bias"].to(f)
+    y = _exact_act(case["act"], z)[0]
+    y = y * st["mul"].to(f) if st["mul"] is not None else y
+    y = y + st["residual"].to(f) if st["residual"] is not None else y
+    return [y.contiguous(), z.contiguous()] if case.get("pre") else [y.contiguous()]
+
+
+def _exact_act(act, z):
+    """The activation and its derivative (by differentiation)."""
+    z = z.detach().requires_grad_(True)
+    if act == "relu":
+        a = z.clamp(min=0)
+    elif act == "gelu":
+        a = z * torch.special.ndtr(z)
+    elif act == "gelu_tanh":
+        a = z * torch.sigmoid(2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3))
+    elif act == "silu":
+        a = z * torch.sigmoid(z)
+    else:
+        a = z * 1.0
+    slope, = torch.autograd.grad(a.sum(), z)
+    return a.detach(), slope
