@@ -24,6 +24,7 @@
 
 #include "bof4.h"
 #include "bof4_device.h"
+#include "bof4_host.h"
 #include "bof4_segment.h"
 #include "bof4_mae.h"
 #include "bof4_gemv.h"
@@ -33,35 +34,6 @@
 
 namespace {
 using namespace bof4;
-
-// ------------------------------------------------------------------------------------------------ host state
-thread_local char g_err[256] = "";
-thread_local int g_hip_err = 0;
-// Caller-owned events to be recorded around the main kernel of the next call (bof4_time_next_call).
-thread_local hipEvent_t g_ev_start = nullptr, g_ev_stop = nullptr;
-void timing_begin(hipStream_t s) {
-    if (g_ev_start) (void)hipEventRecord(g_ev_start, s);
-}
-void timing_end(hipStream_t s) {
-    if (g_ev_stop) (void)hipEventRecord(g_ev_stop, s);
-    g_ev_start = nullptr;
-    g_ev_stop = nullptr;
-}
-
-int fail(int code, const char* msg) {
-    snprintf(g_err, sizeof(g_err), "%s", msg);
-    return code;
-}
-int fail_hip(hipError_t e, const char* where) {
-    g_hip_err = (int)e;
-    snprintf(g_err, sizeof(g_err), "%s: %s", where, hipGetErrorString(e));
-    return BOF4_ERR_HIP;
-}
-#define HIP_TRY(expr)                                  \
-    do {                                               \
-        hipError_t e_ = (expr);                        \
-        if (e_ != hipSuccess) return fail_hip(e_, #expr); \
-    } while (0)
 
 // Device address of a host pointer that the GPU can write (pinned / registered memory), or nullptr for ordinary
 // pageable memory.
@@ -73,36 +45,6 @@ void* device_view_of_host(const void* host_ptr) {
     }
     if (attr.type != hipMemoryTypeHost) return nullptr;
     return attr.devicePointer;
-}
-
-bool valid_block(uint32_t b) { return b == 32 || b == 64 || b == 128 || b == 256; }
-bool valid_codebook(const double* cb) {
-    if (!cb) return false;
-    for (int l = 0; l < 16; ++l)
-        if (!std::isfinite(cb[l])) return false;
-    for (int l = 1; l < 16; ++l)
-        if (!(cb[l] > cb[l - 1])) return false;
-    return true;
-}
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-void make_thresholds(const double* cb, float* thr) {
-    for (int k = 0; k < 15; ++k) {
-        double mid = (cb[k] + cb[k + 1]) * 0.5;
-        float f = (float)mid;  // round to nearest
-        if ((double)f > mid) f = std::nextafterf(f, -INFINITY);
-        thr[k] = f;
-    }
-}
-CodebookArgs make_codebook_args(const double* cb) {
-    CodebookArgs a;
-    make_thresholds(cb, a.thr);
-    a.thr[15] = INFINITY;
-    for (int l = 0; l < 16; ++l) {
-        a.lv32[l] = (float)cb[l];
-        a.cb64[l] = cb[l];
-    }
-    return a;
 }
 
 // Host replica of the kernels' bin index (same fused multiply-add, same mask): monotone in x.
