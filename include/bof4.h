@@ -33,6 +33,10 @@ extern "C" {
 #define BOF4_ERR_HIP (-4)       /* a HIP runtime call failed                                                   */
 
 /* Per-region sums of one Lloyd / EM expectation pass (section 3.2 eq. 6; appendix B.3). */
+/* Element types of tensors that may come in more than one. */
+#define BOF4_F32 0u
+#define BOF4_BF16 1u
+
 typedef struct {
     double num[16];      /* sum over region l of g * x      (numerator of eq. 6)                               */
     double den[16];      /* sum over region l of g          (denominator of eq. 6)                             */
@@ -369,6 +373,48 @@ int bof4_gemm_outlier_table(const uint8_t* codes_dev, const uint16_t* scales_dev
                             const uint16_t* out_val_dev, uint64_t n_outliers, void* table_dev, size_t table_bytes,
                             void* stream);
 size_t bof4_gemm_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t n_tokens);
+
+/*
+ * Log probabilities of given tokens from a model's logits, with the entropy and the largest alternatives of every row:
+ * what the perplexity of section 5 is the exponential of, and what a model is trained and sampled by.  For row i of
+ * n_rows, with p = softmax of its `vocab` logits:
+ *     logprob[i] = log p[target[i]],   entropy[i] = -sum_j p_j log p_j,
+ *     top_idx[i][0 .. top - 1] the ids of the largest logits, descending, of equal ones the lowest id first, and
+ *     top_logprob[i][..] their log probabilities.
+ * Statistics are binary32 whatever the logits' type, in a fixed order: equal calls give equal bits.
+ *   logits_dev  n_rows x vocab of logits_type (BOF4_F32 or BOF4_BF16), row i at element i * ld_logits (>= vocab); any
+ *               alignment of its element's size.  A logit of -inf has no probability and is never an alternative
+ *   target_dev  n_rows ids, or NULL (then logprob_dev is NULL too).  An id below 0 or not below vocab asks for nothing:
+ *               its logprob is 0
+ *   top         0 .. 64 alternatives; a row with fewer logits above -inf has -1 and -inf in the places left over
+ *   entropy_dev, stats_dev   n_rows and n_rows x 2 values, or NULL.  stats: the row's largest logit m and
+ *               log sum_j exp(x_j - m), for bof4_token_logprobs_backward; their sum is the log of the sum of exponentials
+ *   ws_dev      bof4_token_logprobs_workspace_bytes(n_rows, vocab, top) bytes (256-byte aligned); contents undefined after
+ * A row of nothing but -inf: logprob -inf, entropy 0, no alternatives, stats (-inf, 0).  A row that holds a NaN or
+ * +inf: every value of it NaN (but the logprob of no target), no alternatives.  Limits: n_rows < 2^31, vocab <= 2^30.
+ * Only enqueues.
+ */
+int bof4_token_logprobs(const void* logits_dev, uint32_t logits_type, uint64_t n_rows, uint64_t vocab, uint64_t ld_logits,
+                        const int64_t* target_dev, uint32_t top, float* logprob_dev, float* entropy_dev,
+                        int64_t* top_idx_dev, float* top_logprob_dev, float* stats_dev, void* ws_dev, size_t ws_bytes,
+                        void* stream);
+size_t bof4_token_logprobs_workspace_bytes(uint64_t n_rows, uint64_t vocab, uint32_t top);
+
+/*
+ * The gradient of those log probabilities and entropies by the logits: with g = d_logprob[i] and h = d_entropy[i]
+ *     d_logits[i][j] = g * ([j == target[i]] - p_j) - h * p_j * (log p_j + entropy[i]),
+ * p from the logits and the stats that bof4_token_logprobs wrote for them.  (None goes through the alternatives.)
+ *   target_dev and d_logprob_dev   both, or neither (then g = 0); a target that asks for nothing has g = 0 as well
+ *   entropy_dev and d_entropy_dev  both, or neither (then h = 0); entropy as bof4_token_logprobs wrote it
+ *   d_logits_dev  n_rows x vocab of d_logits_type, row stride ld_d_logits (>= vocab), all of it written; may be the logits
+ *               themselves (one type and one row stride)
+ * A logit of -inf and a row of nothing else have a gradient of 0 (the target's own part g aside); a row with a NaN or +inf
+ * has NaN.  Only enqueues.
+ */
+int bof4_token_logprobs_backward(const void* logits_dev, uint32_t logits_type, uint64_t n_rows, uint64_t vocab,
+                                 uint64_t ld_logits, const float* stats_dev, const int64_t* target_dev,
+                                 const float* d_logprob_dev, const float* entropy_dev, const float* d_entropy_dev,
+                                 void* d_logits_dev, uint32_t d_logits_type, uint64_t ld_d_logits, void* stream);
 
 /* Measurement aid: the next bof4_quantize / bof4_dequantize / bof4_lloyd_step / bof4_quant_error / bof4_gemv / bof4_gemm call made by this thread records
  * the caller-owned hipEvent_t `start_event` immediately before and `stop_event` immediately after its main kernel

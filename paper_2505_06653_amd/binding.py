@@ -20,6 +20,7 @@ EXPORTS = ("bof4_workspace_bytes", "bof4_opq_threshold", "bof4_thresholds", "bof
            "bof4_quant_error", "bof4_gemv", "bof4_gemv_outlier_table",
            "bof4_gemv_outlier_table_bytes", "bof4_gemm", "bof4_gemm_pack", "bof4_gemm_packed_bytes",
            "bof4_gemm_outlier_table", "bof4_gemm_workspace_bytes",
+           "bof4_token_logprobs", "bof4_token_logprobs_workspace_bytes", "bof4_token_logprobs_backward",
            "bof4_theory_centroids", "bof4_theory_workspace_bytes", "bof4_time_next_call", "bof4_last_error",
            "bof4_last_hip_error")
 
@@ -134,6 +135,13 @@ def lib():
         L.bof4_gemm_outlier_table.argtypes = L.bof4_gemv_outlier_table.argtypes
         L.bof4_gemm_workspace_bytes.restype = ctypes.c_size_t
         L.bof4_gemm_workspace_bytes.argtypes = [ctypes.c_uint64, ctypes.c_uint64, ctypes.c_uint32]
+        u32, u64, size = ctypes.c_uint32, ctypes.c_uint64, ctypes.c_size_t
+        L.bof4_token_logprobs.restype = ctypes.c_int
+        L.bof4_token_logprobs.argtypes = [vp, u32, u64, u64, u64, vp, u32, vp, vp, vp, vp, vp, vp, size, vp]
+        L.bof4_token_logprobs_workspace_bytes.restype = size
+        L.bof4_token_logprobs_workspace_bytes.argtypes = [u64, u64, u32]
+        L.bof4_token_logprobs_backward.restype = ctypes.c_int
+        L.bof4_token_logprobs_backward.argtypes = [vp, u32, u64, u64, u64, vp, vp, vp, vp, vp, vp, u32, u64, vp]
         L.bof4_theory_workspace_bytes.restype = ctypes.c_size_t
         L.bof4_theory_workspace_bytes.argtypes = [ctypes.c_uint32]
         L.bof4_theory_centroids.restype = ctypes.c_int
@@ -604,4 +612,97 @@ def bof4_dequantize(codes, scales, n, block, cb, out_idx=None, out_val=None, out
         k = int(n_outliers)
     _check(lib().bof4_dequantize(_ptr(codes), _ptr(scales), n, block, cbp, _ptr(out_idx) if k else None,
                                  _ptr(out_val) if k else None, k, _ptr(out), _stream(stream)))
+    return out
+
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1}  # BOF4_F32, BOF4_BF16
+
+
+def _tensor(t, name, dtypes, shape=None, like=None):
+    """A device tensor of one of `dtypes` and of that shape, its last dimension contiguous; on `like`'s device, which has to
+    be the current one (the library enqueues on the current device)."""
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    if not t.is_cuda or (like is not None and t.device != like.device):
+        raise ValueError(f"{name} must be on the same GPU as the other tensors")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    return t
+
+
+def _row_stride(t):
+    """Elements from one row of a 2-d tensor to the next (a single row's stride says nothing)."""
+    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.shape[1]), 1)
+
+
+def _flat(t, name, dtypes, shape, like):
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return _tensor(t, name, dtypes, shape, like)
+
+
+def _scratch(ws, nbytes, like, stream):
+    """The caller's workspace, or one of `nbytes` that the allocator keeps until `stream` is done with it."""
+    if ws is not None:
+        return _flat(ws, "ws", (torch.uint8,), None, like)
+    ws = torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=like.device)
+    if stream is not None:
+        ws.record_stream(stream)
+    return ws
+
+
+def bof4_token_logprobs_workspace_bytes(n_rows, vocab, top=0):
+    return int(lib().bof4_token_logprobs_workspace_bytes(n_rows, vocab, top))
+
+
+def bof4_token_logprobs(logits, targets=None, top=0, ws=None, stream=None):
+    """logits: float32 or bfloat16 [n_rows, vocab] on the device, rows of any stride; targets: int64 [n_rows] (below 0: no
+    token asked for).  Returns (logprob float32 [n_rows] or None without targets, entropy float32 [n_rows], top_idx int64
+    [n_rows, top] and top_logprob float32 [n_rows, top] or None with top = 0, stats float32 [n_rows, 2])."""
+    _tensor(logits, "logits", tuple(_TYPES))
+    if logits.dim() != 2:
+        raise ValueError("logits must be [n_rows, vocab]")
+    n, vocab = logits.shape
+    new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=logits.device)
+    logprob = None
+    if targets is not None:
+        _flat(targets, "targets", (torch.int64,), (n,), logits)
+        logprob = new((n,), torch.float32)
+    entropy, stats = new((n,), torch.float32), new((n, 2), torch.float32)
+    top_idx, top_logprob = (new((n, top), torch.int64), new((n, top), torch.float32)) if top > 0 else (None, None)
+    ws = _scratch(ws, bof4_token_logprobs_workspace_bytes(n, vocab, max(int(top), 0)), logits, stream)
+    _check(lib().bof4_token_logprobs(_ptr(logits), _TYPES[logits.dtype], n, vocab, _row_stride(logits), _ptr(targets),
+                                     int(top), _ptr(logprob), _ptr(entropy), _ptr(top_idx), _ptr(top_logprob), _ptr(stats),
+                                     _ptr(ws), ws.numel(), _stream(stream)))
+    return logprob, entropy, top_idx, top_logprob, stats
+
+
+def bof4_token_logprobs_backward(logits, stats, targets=None, d_logprob=None, entropy=None, d_entropy=None, out=None,
+                                 out_dtype=None, stream=None):
+    """The gradient by the logits, [n_rows, vocab], from bof4_token_logprobs' stats (and entropy) and the gradients of its
+    logprob and entropy (float32 [n_rows]; None: that output is not used).  `out`: a tensor to fill, may be the logits."""
+    _tensor(logits, "logits", tuple(_TYPES))
+    if logits.dim() != 2:
+        raise ValueError("logits must be [n_rows, vocab]")
+    n, vocab = logits.shape
+    f32 = (torch.float32,)
+    _flat(stats, "stats", f32, (n, 2), logits)
+    if (targets is None) != (d_logprob is None) or (entropy is None) != (d_entropy is None):
+        raise ValueError("targets come with d_logprob, the entropy with d_entropy")
+    if targets is not None:
+        _flat(targets, "targets", (torch.int64,), (n,), logits)
+        _flat(d_logprob, "d_logprob", f32, (n,), logits)
+    if entropy is not None:
+        _flat(entropy, "entropy", f32, (n,), logits)
+        _flat(d_entropy, "d_entropy", f32, (n,), logits)
+    if out is None:
+        out = torch.empty((n, vocab), dtype=out_dtype or logits.dtype, device=logits.device)
+    _tensor(out, "out", tuple(_TYPES), (n, vocab), logits)
+    _check(lib().bof4_token_logprobs_backward(_ptr(logits), _TYPES[logits.dtype], n, vocab, _row_stride(logits),
+                                              _ptr(stats), _ptr(targets), _ptr(d_logprob), _ptr(entropy), _ptr(d_entropy),
+                                              _ptr(out), _TYPES[out.dtype], _row_stride(out), _stream(stream)))
     return out

@@ -1,0 +1,94 @@
+// bof4_logprobs.hip - C entries of the token log probabilities and their gradient (include/bof4.h).
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "bof4.h"
+#include "bof4_host.h"
+#include "bof4_logprobs.h"
+
+namespace {
+using namespace bof4;
+
+bool valid_type(uint32_t t) { return t == BOF4_F32 || t == BOF4_BF16; }
+size_t type_bytes(uint32_t t) { return t == BOF4_BF16 ? 2 : 4; }
+constexpr uint64_t LOGPROBS_MAX_ROWS = 0x7fffffffull, LOGPROBS_MAX_VOCAB = 1ull << 30;
+}  // namespace
+
+extern "C" {
+
+size_t bof4_token_logprobs_workspace_bytes(uint64_t n_rows, uint64_t vocab, uint32_t top) {
+    if (n_rows == 0 || vocab == 0 || top > LOGPROBS_MAX_TOP) return 0;
+    return 256;
+}
+
+int bof4_token_logprobs(const void* logits_dev, uint32_t logits_type, uint64_t n_rows, uint64_t vocab, uint64_t ld_logits,
+                        const int64_t* target_dev, uint32_t top, float* logprob_dev, float* entropy_dev,
+                        int64_t* top_idx_dev, float* top_logprob_dev, float* stats_dev, void* ws_dev, size_t ws_bytes,
+                        void* stream) {
+    if (!logits_dev || !ws_dev) return fail(BOF4_ERR_ARG, "bof4_token_logprobs: null pointer");
+    if (!valid_type(logits_type)) return fail(BOF4_ERR_ARG, "bof4_token_logprobs: logits are BOF4_F32 or BOF4_BF16");
+    if (n_rows == 0 || vocab == 0 || n_rows > LOGPROBS_MAX_ROWS || vocab > LOGPROBS_MAX_VOCAB)
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs: 1 to 2^31 - 1 rows and 1 to 2^30 tokens in the vocabulary");
+    if (ld_logits < vocab) return fail(BOF4_ERR_ARG, "bof4_token_logprobs: row stride below the vocabulary");
+    if (!target_dev != !logprob_dev)
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs: targets and their log probabilities come together");
+    if (top > LOGPROBS_MAX_TOP || (top > 0 && (!top_idx_dev || !top_logprob_dev)))
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs: at most 64 alternatives, with both their buffers");
+    if (!aligned(logits_dev, type_bytes(logits_type)) || !aligned(target_dev, 8) || !aligned(logprob_dev, 4) ||
+        !aligned(entropy_dev, 4) || !aligned(top_idx_dev, 8) || !aligned(top_logprob_dev, 4) || !aligned(stats_dev, 4) ||
+        !aligned(ws_dev, 256))
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs: misaligned pointer (its element's size; the workspace 256)");
+    if (ws_bytes < bof4_token_logprobs_workspace_bytes(n_rows, vocab, top))
+        return fail(BOF4_ERR_WORKSPACE, "bof4_token_logprobs: workspace too small");
+    hipStream_t s = (hipStream_t)stream;
+    const LogprobsArgs a = {logits_dev, ld_logits, (uint32_t)n_rows, (uint32_t)vocab, top, target_dev,
+                            logprob_dev, entropy_dev, top_logprob_dev, stats_dev, top_idx_dev};
+    timing_begin(s);
+    if (logits_type == BOF4_BF16) {
+        hipLaunchKernelGGL((logprobs_kernel<true>), dim3(a.n_rows), dim3(256), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((logprobs_kernel<false>), dim3(a.n_rows), dim3(256), 0, s, a);
+    }
+    timing_end(s);
+    HIP_TRY(hipGetLastError());
+    return BOF4_OK;
+}
+
+int bof4_token_logprobs_backward(const void* logits_dev, uint32_t logits_type, uint64_t n_rows, uint64_t vocab,
+                                 uint64_t ld_logits, const float* stats_dev, const int64_t* target_dev,
+                                 const float* d_logprob_dev, const float* entropy_dev, const float* d_entropy_dev,
+                                 void* d_logits_dev, uint32_t d_logits_type, uint64_t ld_d_logits, void* stream) {
+    if (!logits_dev || !stats_dev || !d_logits_dev) return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: null pointer");
+    if (!valid_type(logits_type) || !valid_type(d_logits_type))
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: logits and gradients are BOF4_F32 or BOF4_BF16");
+    if (n_rows == 0 || vocab == 0 || n_rows > LOGPROBS_MAX_ROWS || vocab > LOGPROBS_MAX_VOCAB)
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: 1 to 2^31 - 1 rows and 1 to 2^30 tokens in the vocabulary");
+    if (ld_logits < vocab || ld_d_logits < vocab)
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: row stride below the vocabulary");
+    if (!target_dev != !d_logprob_dev || !entropy_dev != !d_entropy_dev)
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: targets come with d_logprob, the entropy with d_entropy");
+    if (d_logits_dev == logits_dev && (logits_type != d_logits_type || ld_logits != ld_d_logits))
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: in place only with one type and row stride");
+    if (!aligned(logits_dev, type_bytes(logits_type)) || !aligned(d_logits_dev, type_bytes(d_logits_type)) ||
+        !aligned(target_dev, 8) || !aligned(stats_dev, 4) || !aligned(d_logprob_dev, 4) || !aligned(entropy_dev, 4) ||
+        !aligned(d_entropy_dev, 4))
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: misaligned pointer (its element's size)");
+    hipStream_t s = (hipStream_t)stream;
+    const LogprobsGradArgs a = {logits_dev, d_logits_dev, ld_logits, ld_d_logits, (uint32_t)n_rows, (uint32_t)vocab,
+                                target_dev, stats_dev, d_logprob_dev, entropy_dev, d_entropy_dev};
+    const dim3 grid((uint32_t)n_rows, (uint32_t)(vocab < 1024 * 1024 ? (vocab + 1023) / 1024 : 1024));
+    timing_begin(s);
+#define BOF4_LAUNCH_GRAD(IN_, OUT_) hipLaunchKernelGGL((logprobs_grad_kernel<IN_, OUT_>), grid, dim3(256), 0, s, a);
+    if (logits_type == BOF4_BF16) {
+        if (d_logits_type == BOF4_BF16) { BOF4_LAUNCH_GRAD(true, true) } else { BOF4_LAUNCH_GRAD(true, false) }
+    } else {
+        if (d_logits_type == BOF4_BF16) { BOF4_LAUNCH_GRAD(false, true) } else { BOF4_LAUNCH_GRAD(false, false) }
+    }
+#undef BOF4_LAUNCH_GRAD
+    timing_end(s);
+    HIP_TRY(hipGetLastError());
+    return BOF4_OK;
+}
+
+}  // extern "C"
