@@ -257,7 +257,8 @@ def _run_own(case, st):
         logprob, entropy, ids, top, _ = b.bof4_token_logprobs(st["logits"], st["target"], top=case["top"], ws=st["ws"])
         return [logprob, entropy, ids, top] if case["top"] else [logprob, entropy]
     if op == "logprobs_grad":
-        return [b.bof4_token_logprobs_backward(st["logits"], st["stats"], st["target"], st["d_logprob"], st["entropy"],
+        entropy = st["entropy"] if case["entropy"] else None
+        return [b.bof4_token_logprobs_backward(st["logits"], st["stats"], st["target"], st["d_logprob"], entropy,
                                                st["d_entropy"], out=st["out"])]
     rows, cols = case["rows"], case["cols"]
     if op == "few":
