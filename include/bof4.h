@@ -391,7 +391,7 @@ size_t bof4_gemm_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t n_tokens
  *               log sum_j exp(x_j - m), for bof4_token_logprobs_backward; their sum is the log of the sum of exponentials
  *   ws_dev      bof4_token_logprobs_workspace_bytes(n_rows, vocab, top) bytes (256-byte aligned); contents undefined after
  * A row of nothing but -inf: logprob -inf, entropy 0, no alternatives, stats (-inf, 0).  A row that holds a NaN or
- * +inf: every value of it NaN (but the logprob of no target), no alternatives.  Limits: n_rows < 2^31, vocab <= 2^30.
+ * +inf: every value of it NaN (but the logprob of no target), no alternatives.  Limits: n_rows <= 2^23, vocab <= 2^30.
  * Only enqueues.
  */
 int bof4_token_logprobs(const void* logits_dev, uint32_t logits_type, uint64_t n_rows, uint64_t vocab, uint64_t ld_logits,
@@ -409,7 +409,7 @@ size_t bof4_token_logprobs_workspace_bytes(uint64_t n_rows, uint64_t vocab, uint
  *   d_logits_dev  n_rows x vocab of d_logits_type, row stride ld_d_logits (>= vocab), all of it written; may be the logits
  *               themselves (one type and one row stride)
  * A logit of -inf and a row of nothing else have a gradient of 0 (the target's own part g aside); a row with a NaN or +inf
- * has NaN.  Only enqueues.
+ * has NaN.  Limits as above, and fewer than 2^24 stretches of 4096 (binary32) or 8192 (bfloat16) logits.  Only enqueues.
  */
 int bof4_token_logprobs_backward(const void* logits_dev, uint32_t logits_type, uint64_t n_rows, uint64_t vocab,
                                  uint64_t ld_logits, const float* stats_dev, const int64_t* target_dev,

@@ -190,6 +190,29 @@ __device__ __forceinline__ uint32_t wave_inclusive_scan_u32(uint32_t x) {
     return (uint32_t)v;
 }
 
+// Sum over the 64 lanes, delivered in lane 63 (other lanes hold prefixes).  Fixed tree: shifts by 1, 2, 4, 8 inside
+// rows of 16 lanes, then lane 15 of each row into the next odd row, then lane 31 into the upper half.
+__device__ __forceinline__ float wave_sum_lane63(float x) {
+#define BOF4_DPP_F32(v, ctrl, row_mask, bound) \
+    __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, row_mask, 0xf, bound))
+    x += BOF4_DPP_F32(x, 0x111, 0xf, true);
+    x += BOF4_DPP_F32(x, 0x112, 0xf, true);
+    x += BOF4_DPP_F32(x, 0x114, 0xf, true);
+    x += BOF4_DPP_F32(x, 0x118, 0xf, true);
+    x += BOF4_DPP_F32(x, 0x142, 0xa, false);
+    x += BOF4_DPP_F32(x, 0x143, 0xc, false);
+#undef BOF4_DPP_F32
+    return x;
+}
+
+// LDS traffic between the lanes of one wave: the LDS unit serves a wave's requests in order, the fences only
+// keep the compiler from moving the accesses across each other.
+__device__ __forceinline__ void wave_lds_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Slow, always-valid nearest-level search.
 __device__ __forceinline__ int assign_code_generic(float x, const CodebookArgs& cb) {
     int code = 0;

@@ -26,7 +26,6 @@
 #include <cstdint>
 
 #include "bof4_device.h"
-#include "bof4_segment.h"
 #include "bof4_gemv.h"
 #include "bof4_gemm_plan.h"
 

@@ -19,7 +19,6 @@
 #include <cstdint>
 
 #include "bof4_device.h"
-#include "bof4_segment.h"
 
 namespace bof4 {
 
@@ -28,21 +27,6 @@ constexpr uint32_t GEMV_MAX_RC = 64;    // rows per workgroup at most: the last 
 constexpr uint32_t GEMV_MAX_TOKENS = 4;    // tokens per launch: their slices of x live in registers
 constexpr uint32_t GEMV_MAX_STRIPS = 16;  // up to 32768 columns
 constexpr uint32_t GEMV_MAX_WAVES = 8;    // waves per workgroup: two per SIMD, so that several workgroups pack a CU
-
-// Sum over the 64 lanes, delivered in lane 63 (other lanes hold prefixes).  Fixed tree: shifts by 1, 2, 4, 8 inside
-// rows of 16 lanes, then lane 15 of each row into the next odd row, then lane 31 into the upper half.
-__device__ __forceinline__ float wave_sum_lane63(float x) {
-#define BOF4_DPP_F32(v, ctrl, row_mask, bound) \
-    __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, row_mask, 0xf, bound))
-    x += BOF4_DPP_F32(x, 0x111, 0xf, true);
-    x += BOF4_DPP_F32(x, 0x112, 0xf, true);
-    x += BOF4_DPP_F32(x, 0x114, 0xf, true);
-    x += BOF4_DPP_F32(x, 0x118, 0xf, true);
-    x += BOF4_DPP_F32(x, 0x142, 0xa, false);
-    x += BOF4_DPP_F32(x, 0x143, 0xc, false);
-#undef BOF4_DPP_F32
-    return x;
-}
 
 // strip_ptr[r * n_strips + s] = number of list entries with index < r * cols + s * GEMV_STRIP (the list is
 // ascending), for every row and strip, and one closing entry: rows * n_strips + 1 values.

@@ -92,43 +92,301 @@ __device__ __forceinline__ void finish_row(const LogprobsArgs& a, uint32_t row, 
     }
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(256) void logprobs_kernel(LogprobsArgs a) {
-    __shared__ RowSums sums[256];
-    __shared__ uint64_t best[256];
-    const uint32_t tid = threadIdx.x, row = blockIdx.x;
-    const uint64_t base = (uint64_t)row * a.ld;
-    RowSums r = {-INFINITY, 0.0f, 0.0f};
-    for (uint32_t j = tid; j < a.vocab; j += 256) r = merge_sums(r, {load_logit<BF16>(a.logits, base + j), 1.0f, 0.0f});
-    sums[tid] = r;
-    for (uint32_t half = 128; half > 0; half >>= 1) {
-        __syncthreads();
-        if (tid < half) sums[tid] = merge_sums(sums[tid], sums[tid + half]);
-    }
-    uint64_t mine = 0, last = ~0ull;
-    for (uint32_t k = 0; k < a.top; ++k) {
-        uint64_t b = 0;
-        for (uint32_t j = tid; j < a.vocab; j += 256) {
-            const float x = load_logit<BF16>(a.logits, base + j);
-            const uint64_t key = is_alternative(x) ? logit_key(x, j) : 0;
-            if (key < last && key > b) b = key;
-        }
-        __syncthreads();
-        best[tid] = b;
-        for (uint32_t half = 128; half > 0; half >>= 1) {
-            __syncthreads();
-            if (tid < half && best[tid + half] > best[tid]) best[tid] = best[tid + half];
-        }
-        __syncthreads();
-        last = best[0];
-        if (tid == k) mine = last;
-    }
-    __syncthreads();
-    if (tid < 64) finish_row<BF16>(a, row, sums[0], mine, tid);
+// ------------------------------------------------------------------------------------------------ the largest keys
+// The 64 lanes' values exchanged between lanes whose numbers differ in bit D.
+template <int D>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
+    const int x = (int)v;
+    if constexpr (D == 1) return (uint32_t)__builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, true);   // quad_perm 1 0 3 2
+    if constexpr (D == 2) return (uint32_t)__builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, true);   // quad_perm 2 3 0 1
+    if constexpr (D == 4)  // mirrored in eights, then in fours
+        return (uint32_t)__builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true), 0x1b, 0xf, 0xf, true);
+    if constexpr (D == 8) return (uint32_t)__builtin_amdgcn_mov_dpp(x, 0x128, 0xf, 0xf, true);  // rotated by 8 of 16
+    return (uint32_t)__shfl_xor(x, D);
+}
+template <int D>
+__device__ __forceinline__ uint64_t lane_xor64(uint64_t v) {
+    return ((uint64_t)lane_xor<D>((uint32_t)(v >> 32)) << 32) | lane_xor<D>((uint32_t)v);
+}
+// One step of a bitonic network: the larger of a pair goes to the lower lane where `down`.
+template <int D>
+__device__ __forceinline__ uint64_t exchange(uint64_t v, uint32_t lane, bool down) {
+    const uint64_t o = lane_xor64<D>(v);
+    return ((lane & D) == 0u) == down ? (v > o ? v : o) : (v > o ? o : v);
+}
+// Descending order over the lanes of what is already a bitonic sequence of SIZE lanes each.
+template <int SIZE>
+__device__ __forceinline__ uint64_t bitonic_merge(uint64_t v, uint32_t lane, bool down) {
+    if constexpr (SIZE >= 64) v = exchange<32>(v, lane, down);
+    if constexpr (SIZE >= 32) v = exchange<16>(v, lane, down);
+    if constexpr (SIZE >= 16) v = exchange<8>(v, lane, down);
+    if constexpr (SIZE >= 8) v = exchange<4>(v, lane, down);
+    if constexpr (SIZE >= 4) v = exchange<2>(v, lane, down);
+    return exchange<1>(v, lane, down);
+}
+__device__ __forceinline__ uint64_t sort_descending(uint64_t v, uint32_t lane) {
+    v = bitonic_merge<2>(v, lane, (lane & 2u) == 0u);
+    v = bitonic_merge<4>(v, lane, (lane & 4u) == 0u);
+    v = bitonic_merge<8>(v, lane, (lane & 8u) == 0u);
+    v = bitonic_merge<16>(v, lane, (lane & 16u) == 0u);
+    v = bitonic_merge<32>(v, lane, (lane & 32u) == 0u);
+    return bitonic_merge<64>(v, lane, true);
+}
+// The 64 largest of two descending sequences, descending; `reversed`: the second one from the last lane to the first.
+__device__ __forceinline__ uint64_t merge_reversed(uint64_t list, uint64_t reversed, uint32_t lane) {
+    return bitonic_merge<64>(list > reversed ? list : reversed, lane, true);
+}
+__device__ __forceinline__ uint64_t lane_reverse64(uint64_t v, uint32_t lane) {
+    const int at = (int)(63u - lane);
+    return ((uint64_t)(uint32_t)__shfl((int)(v >> 32), at) << 32) | (uint32_t)__shfl((int)(uint32_t)v, at);
+}
+__device__ __forceinline__ uint64_t readlane64(uint64_t v, uint32_t lane) {
+    return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), (int)lane) << 32) |
+           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, (int)lane);
 }
 
-// d x_j = g (delta_jt - p_j) - h p_j (log p_j + H), g and h the gradients of the row's log probability and entropy.  One
-// thread per four logits of a row.
+// ------------------------------------------------------------------------------------------------ a row's pass
+// One pass over the logits.  A wave takes tiles of 256 16-byte words, four to a lane (the next tile's on their way
+// meanwhile), and keeps m, S and T per lane: the maximum moves at most once per tile, and per logit there are a
+// subtraction, an exponential and three more operations.  The lanes and waves join at the end of the row.
+//   The alternatives ride along: a wave knows a bound that its `top` best so far all reach, and only a tile in which some
+// lane's maximum reaches it is looked at again.  Then the tile is parked in LDS, what reaches the bound is collected (as
+// keys that no two logits share) and, 64 at a time, sorted and merged into the wave's sorted list, one key to a lane.
+// Before a tile with many such lanes is collected the bound is raised to what at least `top` lanes' maxima reach (their
+// highest 16 bits, by bisection), so that the first tile does not bring a thousand candidates.  Every element that is
+// left out is smaller than `top` others, so the result does not depend on how the row was cut.
+//   With few rows a row is cut into n_splits parts, one per workgroup, whose records logprobs_join_kernel joins.
+constexpr uint32_t LOGPROBS_WAVES = 4, LOGPROBS_WORDS = 4;             // per workgroup; 16-byte words per lane and tile
+constexpr uint32_t LOGPROBS_TILE = 64 * LOGPROBS_WORDS;                // words
+constexpr uint32_t LOGPROBS_MAX_SPLITS = 64, LOGPROBS_TARGET_WGS = 1024;
+constexpr uint32_t logprobs_word_elements(bool bf16) { return bf16 ? 8 : 4; }
+
+struct LogprobsPart {  // what a part of a row leaves: its sums, then `top` keys
+    RowSums r;
+    uint32_t unused;
+};
+__device__ __forceinline__ LogprobsPart* logprobs_part(char* ws, uint64_t at, uint32_t top) {
+    return reinterpret_cast<LogprobsPart*>(ws + at * (sizeof(LogprobsPart) + 8ull * top));
+}
+
+template <int D>
+__device__ __forceinline__ RowSums join_step(RowSums r) {
+    const RowSums o = {__uint_as_float(lane_xor<D>(__float_as_uint(r.m))), __uint_as_float(lane_xor<D>(__float_as_uint(r.s))),
+                       __uint_as_float(lane_xor<D>(__float_as_uint(r.t)))};
+    return merge_sums(r, o);
+}
+// All lanes' sums joined, as the first lane has them, in every lane.
+__device__ __forceinline__ RowSums join_lanes(RowSums r) {
+    r = join_step<32>(join_step<16>(join_step<8>(join_step<4>(join_step<2>(join_step<1>(r))))));
+    return {__uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(r.m))),
+            __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(r.s))),
+            __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(r.t)))};
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(64 * LOGPROBS_WAVES) void logprobs_kernel(LogprobsArgs a, uint32_t n_splits,
+                                                                       uint32_t tiles_per_split, char* ws) {
+    constexpr uint32_t PER_WORD = logprobs_word_elements(BF16), SIZE = BF16 ? 2 : 4;
+    struct Shared {
+        uint4 tile[LOGPROBS_WAVES][LOGPROBS_TILE];
+        uint64_t found[LOGPROBS_WAVES][128];
+        RowSums sums[LOGPROBS_WAVES];
+        uint64_t list[LOGPROBS_WAVES][64];
+    };
+    __shared__ __attribute__((aligned(16))) Shared sh;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t row = blockIdx.x / n_splits, split = blockIdx.x - row * n_splits;
+    // The row in 16-byte words of memory: the first and the last may hold logits of other rows or none, and only
+    // the row's own are read of those two.
+    const char* row_ptr = static_cast<const char*>(a.logits) + (uint64_t)row * a.ld * SIZE;
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(row_ptr) & 15u) / SIZE;  // logits in front of the row's first
+    const char* words = row_ptr - off * SIZE;
+    const uint32_t end = off + a.vocab, n_words = (end + PER_WORD - 1) / PER_WORD;
+    const uint32_t n_tiles = (n_words + LOGPROBS_TILE - 1) / LOGPROBS_TILE;
+    const uint32_t tile0 = split * tiles_per_split, tile1 = min(n_tiles, tile0 + tiles_per_split);
+
+    struct Tile {
+        uint4 q[LOGPROBS_WORDS];
+    };
+    auto fetch = [&](uint32_t tile) __attribute__((always_inline)) {
+        Tile t;
+        const uint32_t w0 = tile * LOGPROBS_TILE + lane;
+        if (tile > 0 && (tile + 1) * LOGPROBS_TILE * PER_WORD <= end) {  // whole words only
+#pragma unroll
+            for (uint32_t k = 0; k < LOGPROBS_WORDS; ++k) t.q[k] = load_stream(reinterpret_cast<const uint4*>(words) + w0 + 64 * k);
+            return t;
+        }
+        constexpr uint32_t NONE = BF16 ? 0xff80ff80u : 0xff800000u;  // -inf
+#pragma unroll
+        for (uint32_t k = 0; k < LOGPROBS_WORDS; ++k) {
+            const uint32_t w = w0 + 64 * k, first = w * PER_WORD;
+            if (first >= off && first + PER_WORD <= end) {
+                t.q[k] = reinterpret_cast<const uint4*>(words)[w];
+                continue;
+            }
+            uint32_t v[4] = {NONE, NONE, NONE, NONE};
+#pragma unroll
+            for (uint32_t i = 0; i < PER_WORD; ++i) {
+                if (first + i < off || first + i >= end) continue;
+                if constexpr (BF16) {
+                    const uint32_t x = reinterpret_cast<const uint16_t*>(words)[first + i];
+                    v[i / 2] = i % 2 ? (v[i / 2] & 0xffffu) | (x << 16) : (v[i / 2] & 0xffff0000u) | x;
+                } else {
+                    v[i] = reinterpret_cast<const uint32_t*>(words)[first + i];
+                }
+            }
+            t.q[k] = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+        return t;
+    };
+
+    float m = -INFINITY, s0 = 0.0f, s1 = 0.0f, t0 = 0.0f, t1 = 0.0f;
+    uint64_t list = 0;                     // the wave's best, descending over the lanes
+    float bound = -3.4028234663852886e38f;  // what a logit has to reach to matter (the lowest number: any but -inf)
+    float last_of_list = bound;             // the `top`-th best so far
+    uint32_t n_found = 0;
+    uint64_t* found = sh.found[wave];
+    auto drain = [&]() {  // the first 64 of what was collected go into the list
+        wave_lds_fence();
+        const uint64_t v = lane < n_found ? found[lane] : 0;
+        const uint64_t rest = 64 + lane < n_found ? found[64 + lane] : 0;
+        wave_lds_fence();
+        if (64 + lane < n_found) found[lane] = rest;
+        n_found = n_found > 64 ? n_found - 64 : 0;
+        list = merge_reversed(list, lane_reverse64(sort_descending(v, lane), lane), lane);
+        const uint64_t last = readlane64(list, a.top - 1);
+        if (last != 0) {
+            last_of_list = key_logit(last);
+            bound = fmaxf(bound, key_logit(last + (1ull << 32)));  // more than that: what comes later has a higher id
+        }
+    };
+    auto collect = [&](const Tile& t, uint32_t tile, float lane_max, uint64_t reach) {
+        float least = bound;
+        if (__popcll(reach) > a.top) {  // what `top` lanes' maxima reach, in their highest 16 bits
+            const uint32_t key = lane_max >= bound ? (uint32_t)(logit_key(lane_max, 0) >> 48) : 0u;
+            uint32_t b = 0;
+            for (uint32_t bit = 0x8000u; bit != 0; bit >>= 1)
+                if ((uint32_t)__popcll(__builtin_amdgcn_ballot_w64(key >= (b | bit))) >= a.top) b |= bit;
+            least = fmaxf(least, key_logit((uint64_t)b << 48));
+        }
+        uint4* parked = sh.tile[wave];
+#pragma unroll
+        for (uint32_t k = 0; k < LOGPROBS_WORDS; ++k) parked[64 * k + lane] = t.q[k];
+        wave_lds_fence();
+        for (uint32_t i = 0; i < LOGPROBS_WORDS * PER_WORD; ++i) {
+            const uint32_t word = 64 * (i / PER_WORD) + lane;
+            const float x = load_logit<BF16>(parked, word * PER_WORD + i % PER_WORD);
+            const bool take = x >= least;
+            const uint64_t mask = __builtin_amdgcn_ballot_w64(take);
+            if (mask == 0) continue;
+            const uint32_t at = n_found + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+            if (take) found[at] = logit_key(x, (tile * LOGPROBS_TILE + word) * PER_WORD + i % PER_WORD - off);
+            n_found += (uint32_t)__popcll(mask);
+            if (n_found >= 64) {
+                drain();
+                least = fmaxf(least, last_of_list);  // (an equal one with a lower id may follow within the tile)
+            }
+        }
+        wave_lds_fence();
+    };
+    auto add = [&](const Tile& t, uint32_t tile) __attribute__((always_inline)) {
+        float x[LOGPROBS_WORDS * PER_WORD];
+#pragma unroll
+        for (uint32_t k = 0; k < LOGPROBS_WORDS; ++k) {
+            const uint32_t w[4] = {t.q[k].x, t.q[k].y, t.q[k].z, t.q[k].w};
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                if constexpr (BF16) {
+                    x[8 * k + 2 * i] = __uint_as_float(w[i] << 16);
+                    x[8 * k + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+                } else {
+                    x[4 * k + i] = __uint_as_float(w[i]);
+                }
+            }
+        }
+        float lane_max = x[0];
+#pragma unroll
+        for (uint32_t i = 1; i < LOGPROBS_WORDS * PER_WORD; ++i) lane_max = fmaxf(lane_max, x[i]);
+        const float m_new = fmaxf(m, lane_max), ms = finite_max(m_new);
+        const float moved = m - ms, f = logprobs_exp(moved), moved_f = fmaxf(moved, -1e30f);
+        t0 = f * fmaf(s0, moved_f, t0);
+        t1 = f * fmaf(s1, moved_f, t1);
+        s0 *= f;
+        s1 *= f;
+        m = m_new;
+#pragma unroll
+        for (uint32_t i = 0; i < LOGPROBS_WORDS * PER_WORD; i += 2) {
+            const float u0 = x[i] - ms, u1 = x[i + 1] - ms, e0 = logprobs_exp(u0), e1 = logprobs_exp(u1);
+            s0 += e0;
+            s1 += e1;
+            t0 = fmaf(e0, fmaxf(u0, -1e30f), t0);
+            t1 = fmaf(e1, fmaxf(u1, -1e30f), t1);
+        }
+        if (a.top > 0) {
+            const uint64_t reach = __builtin_amdgcn_ballot_w64(lane_max >= bound);
+            if (reach != 0) collect(t, tile, lane_max, reach);
+        }
+    };
+    uint32_t tile = tile0 + wave;
+    if (tile < tile1) {
+        Tile now = fetch(tile);
+        for (; tile < tile1; tile += LOGPROBS_WAVES) {
+            Tile next = now;
+            if (tile + LOGPROBS_WAVES < tile1) next = fetch(tile + LOGPROBS_WAVES);
+            __builtin_amdgcn_sched_barrier(0);
+            add(now, tile);
+            now = next;
+        }
+    }
+    if (a.top > 0 && n_found > 0) drain();
+    // lanes, then waves, in a fixed order
+    RowSums r = {m, s0 + s1, t0 + t1};
+    r = join_lanes(r);
+    if (lane == 0) sh.sums[wave] = r;
+    if (a.top > 0) sh.list[wave][lane] = list;
+    __syncthreads();
+    if (wave != 0) return;
+    r = sh.sums[0];
+    for (uint32_t w = 1; w < LOGPROBS_WAVES; ++w) r = merge_sums(r, sh.sums[w]);
+    if (a.top > 0)
+        for (uint32_t w = 1; w < LOGPROBS_WAVES; ++w) list = merge_reversed(list, sh.list[w][63 - lane], lane);
+    if (n_splits == 1) {
+        finish_row<BF16>(a, row, r, list, lane);
+        return;
+    }
+    LogprobsPart* part = logprobs_part(ws, blockIdx.x, a.top);
+    if (lane == 0) part->r = r;
+    if (lane < a.top) reinterpret_cast<uint64_t*>(part + 1)[lane] = list;
+}
+
+// A row from the records of its parts, in their order: one workgroup per row, whose waves take the parts in turn.
+template <bool BF16>
+__global__ __launch_bounds__(64 * LOGPROBS_WAVES) void logprobs_join_kernel(LogprobsArgs a, uint32_t n_splits, char* ws) {
+    __shared__ uint64_t lists[LOGPROBS_WAVES][64];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = blockIdx.x;
+    const uint64_t first = (uint64_t)row * n_splits;
+    uint64_t list = 0;
+    if (a.top > 0) {
+        for (uint32_t p = wave; p < n_splits; p += LOGPROBS_WAVES) {
+            const uint64_t* keys = reinterpret_cast<const uint64_t*>(logprobs_part(ws, first + p, a.top) + 1);
+            const uint32_t at = 63 - lane;
+            list = merge_reversed(list, at < a.top ? keys[at] : 0, lane);
+        }
+        lists[wave][lane] = list;
+        __syncthreads();
+    }
+    if (wave != 0) return;
+    if (a.top > 0)
+        for (uint32_t w = 1; w < LOGPROBS_WAVES; ++w) list = merge_reversed(list, lists[w][63 - lane], lane);
+    RowSums r = {-INFINITY, 0.0f, 0.0f};
+    if (lane < n_splits) r = logprobs_part(ws, first + lane, a.top)->r;
+    r = join_lanes(r);
+    finish_row<BF16>(a, row, r, list, lane);
+}
+
+// d x_j = g (delta_jt - p_j) - h p_j (log p_j + H), g and h the gradients of the row's log probability and entropy: read
+// once, written once.  A workgroup takes a stretch of a row, in 16-byte words of the logits as they lie in memory; their
+// gradients leave in wide stores where the output's rows are aligned alike.
 struct LogprobsGradArgs {
     const void* logits;
     void* out;
@@ -137,23 +395,89 @@ struct LogprobsGradArgs {
     const int64_t* target;
     const float *stats, *d_logprob, *entropy, *d_entropy;
 };
-template <bool BF16, bool OUT_BF16>
-__global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobsGradArgs a) {
-    const uint32_t row = blockIdx.x;
+constexpr uint32_t LOGPROBS_GRAD_WORDS = 4;  // 16-byte words per thread
+template <bool BF16, bool OUT_BF16, bool ENTROPY>
+__global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobsGradArgs a, uint32_t stretches) {
+    constexpr uint32_t PER_WORD = logprobs_word_elements(BF16), SIZE = BF16 ? 2 : 4, OUT_SIZE = OUT_BF16 ? 2 : 4;
+    const uint32_t row = blockIdx.x / stretches, stretch = blockIdx.x - row * stretches;
+    const char* row_ptr = static_cast<const char*>(a.logits) + (uint64_t)row * a.ld * SIZE;
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(row_ptr) & 15u) / SIZE;
+    const char* words = row_ptr - off * SIZE;
+    const uint32_t end = off + a.vocab, n_words = (end + PER_WORD - 1) / PER_WORD;
+    const uint32_t w0 = stretch * 256 * LOGPROBS_GRAD_WORDS + threadIdx.x;
+    char* out = static_cast<char*>(a.out) + (uint64_t)row * a.ld_out * OUT_SIZE - (uint64_t)off * OUT_SIZE;
+    const bool wide = (reinterpret_cast<uintptr_t>(out) & (PER_WORD * OUT_SIZE < 16 ? PER_WORD * OUT_SIZE - 1 : 15u)) == 0u;
     const float m = a.stats[2 * (uint64_t)row], log_s = a.stats[2 * (uint64_t)row + 1];
     const int64_t t = a.target ? a.target[row] : -1;
     const bool asked = t >= 0 && t < (int64_t)a.vocab;
-    const float g = asked && a.d_logprob ? a.d_logprob[row] : 0.0f;
-    const float h = a.d_entropy ? a.d_entropy[row] : 0.0f, H = a.d_entropy ? a.entropy[row] : 0.0f;
+    const float g = asked ? a.d_logprob[row] : 0.0f;
+    const uint32_t target = asked ? off + (uint32_t)t : 0xffffffffu;
+    const float h = ENTROPY ? a.d_entropy[row] : 0.0f, H = ENTROPY ? a.entropy[row] : 0.0f;
     const bool nothing = m == -INFINITY && log_s == 0.0f;
-    for (uint32_t j = blockIdx.y * 256 + threadIdx.x; j < a.vocab; j += gridDim.y * 256) {
-        const float lp = (load_logit<BF16>(a.logits, (uint64_t)row * a.ld + j) - finite_max(m)) - log_s;
-        const float p = logprobs_exp(lp);
-        float d = -p * fmaf(h, fmaxf(lp, -1e30f) + H, g);
-        if (asked && j == (uint32_t)t) d += g;
+    const float ms = finite_max(m);
+    auto slope = [&](float x) __attribute__((always_inline)) {
+        const float lp = (x - ms) - log_s, p = logprobs_exp(lp);
+        return ENTROPY ? -p * fmaf(h, fmaxf(lp, -1e30f) + H, g) : -p * g;
+    };
+    auto one = [&](uint32_t j) {  // j counted from the first word, as `target`
+        const float x = load_logit<BF16>(words, j);
+        float d = slope(x);
+        if (j == target) d += g;
         if (nothing) d = 0.0f;
-        if constexpr (OUT_BF16) reinterpret_cast<uint16_t*>(a.out)[(uint64_t)row * a.ld_out + j] = (uint16_t)f32_to_bf16_rne(d);
-        else reinterpret_cast<float*>(a.out)[(uint64_t)row * a.ld_out + j] = d;
+        if constexpr (OUT_BF16) reinterpret_cast<uint16_t*>(out)[j] = (uint16_t)f32_to_bf16_rne(d);
+        else reinterpret_cast<float*>(out)[j] = d;
+    };
+    uint4 q[LOGPROBS_GRAD_WORDS];
+    bool whole[LOGPROBS_GRAD_WORDS];
+#pragma unroll
+    for (uint32_t k = 0; k < LOGPROBS_GRAD_WORDS; ++k) {
+        const uint32_t w = w0 + 256 * k, first = w * PER_WORD;
+        whole[k] = w < n_words && first >= off && first + PER_WORD <= end;
+        if (whole[k]) q[k] = load_stream(reinterpret_cast<const uint4*>(words) + w);
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < LOGPROBS_GRAD_WORDS; ++k) {
+        const uint32_t w = w0 + 256 * k, first = w * PER_WORD;
+        if (!whole[k]) {
+            if (w < n_words)
+                for (uint32_t j = first < off ? off : first; j < end && j < first + PER_WORD; ++j) one(j);
+            continue;
+        }
+        const uint32_t v[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+        float d[PER_WORD];
+#pragma unroll
+        for (uint32_t i = 0; i < PER_WORD; ++i) {
+            float x;
+            if constexpr (BF16) x = i % 2 ? __uint_as_float(v[i / 2] & 0xffff0000u) : __uint_as_float(v[i / 2] << 16);
+            else x = __uint_as_float(v[i]);
+            d[i] = nothing ? 0.0f : slope(x);
+        }
+        if (target - first < PER_WORD) {
+#pragma unroll
+            for (uint32_t i = 0; i < PER_WORD; ++i)
+                if (first + i == target && !nothing) d[i] += g;
+        }
+        if (!wide) {
+#pragma unroll
+            for (uint32_t i = 0; i < PER_WORD; ++i) {
+                if constexpr (OUT_BF16) reinterpret_cast<uint16_t*>(out)[first + i] = (uint16_t)f32_to_bf16_rne(d[i]);
+                else reinterpret_cast<float*>(out)[first + i] = d[i];
+            }
+            continue;
+        }
+        char* to = out + (uint64_t)first * OUT_SIZE;
+        if constexpr (OUT_BF16) {
+            uint32_t o[PER_WORD / 2];
+#pragma unroll
+            for (uint32_t i = 0; i < PER_WORD / 2; ++i) o[i] = f32_to_bf16_rne(d[2 * i]) | (f32_to_bf16_rne(d[2 * i + 1]) << 16);
+            if constexpr (PER_WORD == 8) store_stream(reinterpret_cast<uint4*>(to), make_uint4(o[0], o[1], o[2], o[3]));
+            else *reinterpret_cast<uint2*>(to) = make_uint2(o[0], o[1]);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < PER_WORD; i += 4)
+                store_stream(reinterpret_cast<uint4*>(to) + i / 4, make_uint4(__float_as_uint(d[i]), __float_as_uint(d[i + 1]),
+                                                                            __float_as_uint(d[i + 2]), __float_as_uint(d[i + 3])));
+        }
     }
 }
 

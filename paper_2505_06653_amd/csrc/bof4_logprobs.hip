@@ -4,6 +4,7 @@
 #include <cstdint>
 
 #include "bof4.h"
+#include "bof4_gemm_plan.h"
 #include "bof4_host.h"
 #include "bof4_logprobs.h"
 
@@ -12,14 +13,30 @@ using namespace bof4;
 
 bool valid_type(uint32_t t) { return t == BOF4_F32 || t == BOF4_BF16; }
 size_t type_bytes(uint32_t t) { return t == BOF4_BF16 ? 2 : 4; }
-constexpr uint64_t LOGPROBS_MAX_ROWS = 0x7fffffffull, LOGPROBS_MAX_VOCAB = 1ull << 30;
+constexpr uint64_t LOGPROBS_MAX_ROWS = 1ull << 23, LOGPROBS_MAX_VOCAB = 1ull << 30;  // (a launch holds fewer than 2^32 lanes)
+
+// Parts per row: with fewer rows than workgroups wanted, as many as give every wave a tile.
+struct LogprobsCut {
+    uint32_t splits, tiles_per_split;
+};
+LogprobsCut logprobs_cut(uint64_t n_rows, uint64_t vocab, bool bf16) {
+    const uint64_t per_word = logprobs_word_elements(bf16), words = (vocab + 2 * per_word - 2) / per_word;  // wherever it begins
+    const uint64_t tiles = (words + LOGPROBS_TILE - 1) / LOGPROBS_TILE;
+    uint64_t splits = (LOGPROBS_TARGET_WGS + n_rows - 1) / n_rows;
+    if (splits > LOGPROBS_MAX_SPLITS) splits = LOGPROBS_MAX_SPLITS;
+    uint64_t per = (tiles + splits - 1) / splits;
+    if (per < LOGPROBS_WAVES) per = LOGPROBS_WAVES;
+    return {(uint32_t)((tiles + per - 1) / per), (uint32_t)per};
+}
 }  // namespace
 
 extern "C" {
 
 size_t bof4_token_logprobs_workspace_bytes(uint64_t n_rows, uint64_t vocab, uint32_t top) {
-    if (n_rows == 0 || vocab == 0 || top > LOGPROBS_MAX_TOP) return 0;
-    return 256;
+    if (n_rows == 0 || vocab == 0 || top > LOGPROBS_MAX_TOP || n_rows > LOGPROBS_MAX_ROWS || vocab > LOGPROBS_MAX_VOCAB) return 0;
+    const uint32_t f32 = logprobs_cut(n_rows, vocab, false).splits, bf16 = logprobs_cut(n_rows, vocab, true).splits;
+    const uint64_t most = f32 > bf16 ? f32 : bf16;
+    return most > 1 ? align_up(n_rows * most * (sizeof(LogprobsPart) + 8 * top), 256) : 256;
 }
 
 int bof4_token_logprobs(const void* logits_dev, uint32_t logits_type, uint64_t n_rows, uint64_t vocab, uint64_t ld_logits,
@@ -29,7 +46,7 @@ int bof4_token_logprobs(const void* logits_dev, uint32_t logits_type, uint64_t n
     if (!logits_dev || !ws_dev) return fail(BOF4_ERR_ARG, "bof4_token_logprobs: null pointer");
     if (!valid_type(logits_type)) return fail(BOF4_ERR_ARG, "bof4_token_logprobs: logits are BOF4_F32 or BOF4_BF16");
     if (n_rows == 0 || vocab == 0 || n_rows > LOGPROBS_MAX_ROWS || vocab > LOGPROBS_MAX_VOCAB)
-        return fail(BOF4_ERR_ARG, "bof4_token_logprobs: 1 to 2^31 - 1 rows and 1 to 2^30 tokens in the vocabulary");
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs: 1 to 2^23 rows and 1 to 2^30 tokens in the vocabulary");
     if (ld_logits < vocab) return fail(BOF4_ERR_ARG, "bof4_token_logprobs: row stride below the vocabulary");
     if (!target_dev != !logprob_dev)
         return fail(BOF4_ERR_ARG, "bof4_token_logprobs: targets and their log probabilities come together");
@@ -44,13 +61,23 @@ int bof4_token_logprobs(const void* logits_dev, uint32_t logits_type, uint64_t n
     hipStream_t s = (hipStream_t)stream;
     const LogprobsArgs a = {logits_dev, ld_logits, (uint32_t)n_rows, (uint32_t)vocab, top, target_dev,
                             logprob_dev, entropy_dev, top_logprob_dev, stats_dev, top_idx_dev};
+    const bool bf16 = logits_type == BOF4_BF16;
+    const LogprobsCut cut = logprobs_cut(n_rows, vocab, bf16);
+    const dim3 grid(a.n_rows * cut.splits), threads(64 * LOGPROBS_WAVES);
     timing_begin(s);
-    if (logits_type == BOF4_BF16) {
-        hipLaunchKernelGGL((logprobs_kernel<true>), dim3(a.n_rows), dim3(256), 0, s, a);
+    if (bf16) {
+        hipLaunchKernelGGL((logprobs_kernel<true>), grid, threads, 0, s, a, cut.splits, cut.tiles_per_split, (char*)ws_dev);
     } else {
-        hipLaunchKernelGGL((logprobs_kernel<false>), dim3(a.n_rows), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((logprobs_kernel<false>), grid, threads, 0, s, a, cut.splits, cut.tiles_per_split, (char*)ws_dev);
     }
     timing_end(s);
+    if (cut.splits > 1) {
+        if (bf16) {
+            hipLaunchKernelGGL((logprobs_join_kernel<true>), dim3(a.n_rows), threads, 0, s, a, cut.splits, (char*)ws_dev);
+        } else {
+            hipLaunchKernelGGL((logprobs_join_kernel<false>), dim3(a.n_rows), threads, 0, s, a, cut.splits, (char*)ws_dev);
+        }
+    }
     HIP_TRY(hipGetLastError());
     return BOF4_OK;
 }
@@ -63,7 +90,7 @@ int bof4_token_logprobs_backward(const void* logits_dev, uint32_t logits_type, u
     if (!valid_type(logits_type) || !valid_type(d_logits_type))
         return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: logits and gradients are BOF4_F32 or BOF4_BF16");
     if (n_rows == 0 || vocab == 0 || n_rows > LOGPROBS_MAX_ROWS || vocab > LOGPROBS_MAX_VOCAB)
-        return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: 1 to 2^31 - 1 rows and 1 to 2^30 tokens in the vocabulary");
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: 1 to 2^23 rows and 1 to 2^30 tokens in the vocabulary");
     if (ld_logits < vocab || ld_d_logits < vocab)
         return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: row stride below the vocabulary");
     if (!target_dev != !d_logprob_dev || !entropy_dev != !d_entropy_dev)
@@ -77,10 +104,20 @@ int bof4_token_logprobs_backward(const void* logits_dev, uint32_t logits_type, u
     hipStream_t s = (hipStream_t)stream;
     const LogprobsGradArgs a = {logits_dev, d_logits_dev, ld_logits, ld_d_logits, (uint32_t)n_rows, (uint32_t)vocab,
                                 target_dev, stats_dev, d_logprob_dev, entropy_dev, d_entropy_dev};
-    const dim3 grid((uint32_t)n_rows, (uint32_t)(vocab < 1024 * 1024 ? (vocab + 1023) / 1024 : 1024));
+    const bool bf16 = logits_type == BOF4_BF16;
+    const uint64_t per_word = logprobs_word_elements(bf16), words = (vocab + 2 * per_word - 2) / per_word;  // wherever a row begins
+    const uint64_t stretches = (words + 256 * LOGPROBS_GRAD_WORDS - 1) / (256 * LOGPROBS_GRAD_WORDS);
+    if (n_rows * stretches >= 1ull << 24)
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: 2^24 and more stretches of 4096 (binary32) or 8192 logits");
+    const dim3 grid((uint32_t)(n_rows * stretches));
     timing_begin(s);
-#define BOF4_LAUNCH_GRAD(IN_, OUT_) hipLaunchKernelGGL((logprobs_grad_kernel<IN_, OUT_>), grid, dim3(256), 0, s, a);
-    if (logits_type == BOF4_BF16) {
+#define BOF4_LAUNCH_GRAD(IN_, OUT_)                                                                                     \
+    if (d_entropy_dev) {                                                                                               \
+        hipLaunchKernelGGL((logprobs_grad_kernel<IN_, OUT_, true>), grid, dim3(256), 0, s, a, (uint32_t)stretches);     \
+    } else {                                                                                                           \
+        hipLaunchKernelGGL((logprobs_grad_kernel<IN_, OUT_, false>), grid, dim3(256), 0, s, a, (uint32_t)stretches);    \
+    }
+    if (bf16) {
         if (d_logits_type == BOF4_BF16) { BOF4_LAUNCH_GRAD(true, true) } else { BOF4_LAUNCH_GRAD(true, false) }
     } else {
         if (d_logits_type == BOF4_BF16) { BOF4_LAUNCH_GRAD(false, true) } else { BOF4_LAUNCH_GRAD(false, false) }

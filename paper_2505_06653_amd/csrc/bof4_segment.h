@@ -65,14 +65,6 @@ __device__ __forceinline__ void tile_fetch(const char* stage, uint32_t lane, uin
         R[4 * i + 3] = q.w;
     }
 }
-// LDS traffic between the lanes of one wave: the LDS unit serves a wave's requests in order, the fences only
-// keep the compiler from moving the accesses across each other.
-__device__ __forceinline__ void wave_lds_fence() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 template <int WIDTH>
 __device__ __forceinline__ int group_max_i32(int v) {
 #pragma unroll
