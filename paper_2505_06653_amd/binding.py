@@ -618,20 +618,18 @@ def bof4_dequantize(codes, scales, n, block, cb, out_idx=None, out_val=None, out
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}  # BOF4_F32, BOF4_BF16
 
 
-def _tensor(t, name, dtypes, shape=None, like=None):
-    """A device tensor of one of `dtypes` and of that shape, its last dimension contiguous; on `like`'s device, which has to
-    be the current one (the library enqueues on the current device)."""
+def _tensor(t, name, dtypes, shape=None):
+    """A device tensor of one of `dtypes` and of that shape, its last dimension contiguous, on the current device (the
+    library enqueues on that).  Returns its address."""
     if t.dtype not in dtypes:
         raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
-    if not t.is_cuda or (like is not None and t.device != like.device):
-        raise ValueError(f"{name} must be on the same GPU as the other tensors")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current device")
-    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current GPU, not on {t.device}")
+    if not t.is_contiguous() and t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name} must be contiguous in its last dimension")
-    return t
+    return t.data_ptr()
 
 
 def _row_stride(t):
@@ -639,17 +637,21 @@ def _row_stride(t):
     return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.shape[1]), 1)
 
 
-def _flat(t, name, dtypes, shape, like):
+def _flat(t, name, dtypes, shape=None):
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    return _tensor(t, name, dtypes, shape, like)
+    return _tensor(t, name, dtypes, shape)
 
 
-def _scratch(ws, nbytes, like, stream):
+_F32, _I64, _U8 = (torch.float32,), (torch.int64,), (torch.uint8,)
+
+
+def _scratch(ws, nbytes, device, stream):
     """The caller's workspace, or one of `nbytes` that the allocator keeps until `stream` is done with it."""
     if ws is not None:
-        return _flat(ws, "ws", (torch.uint8,), None, like)
-    ws = torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=like.device)
+        _flat(ws, "ws", _U8)
+        return ws
+    ws = torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
     if stream is not None:
         ws.record_stream(stream)
     return ws
@@ -663,21 +665,27 @@ def bof4_token_logprobs(logits, targets=None, top=0, ws=None, stream=None):
     """logits: float32 or bfloat16 [n_rows, vocab] on the device, rows of any stride; targets: int64 [n_rows] (below 0: no
     token asked for).  Returns (logprob float32 [n_rows] or None without targets, entropy float32 [n_rows], top_idx int64
     [n_rows, top] and top_logprob float32 [n_rows, top] or None with top = 0, stats float32 [n_rows, 2])."""
-    _tensor(logits, "logits", tuple(_TYPES))
+    logits_at = _tensor(logits, "logits", _TYPES)
     if logits.dim() != 2:
         raise ValueError("logits must be [n_rows, vocab]")
     n, vocab = logits.shape
-    new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=logits.device)
-    logprob = None
+    dev, f32, top = logits.device, torch.float32, int(top)
+    if top < 0:
+        raise ValueError("top must not be negative")
+    logprob = top_idx = top_logprob = targets_at = logprob_at = idx_at = top_at = None
     if targets is not None:
-        _flat(targets, "targets", (torch.int64,), (n,), logits)
-        logprob = new((n,), torch.float32)
-    entropy, stats = new((n,), torch.float32), new((n, 2), torch.float32)
-    top_idx, top_logprob = (new((n, top), torch.int64), new((n, top), torch.float32)) if top > 0 else (None, None)
-    ws = _scratch(ws, bof4_token_logprobs_workspace_bytes(n, vocab, max(int(top), 0)), logits, stream)
-    _check(lib().bof4_token_logprobs(_ptr(logits), _TYPES[logits.dtype], n, vocab, _row_stride(logits), _ptr(targets),
-                                     int(top), _ptr(logprob), _ptr(entropy), _ptr(top_idx), _ptr(top_logprob), _ptr(stats),
-                                     _ptr(ws), ws.numel(), _stream(stream)))
+        targets_at = _flat(targets, "targets", _I64, (n,))
+        logprob = torch.empty(n, dtype=f32, device=dev)
+        logprob_at = logprob.data_ptr()
+    entropy, stats = torch.empty(n, dtype=f32, device=dev), torch.empty((n, 2), dtype=f32, device=dev)
+    if top > 0:
+        top_idx = torch.empty((n, top), dtype=torch.int64, device=dev)
+        top_logprob = torch.empty((n, top), dtype=f32, device=dev)
+        idx_at, top_at = top_idx.data_ptr(), top_logprob.data_ptr()
+    ws = _scratch(ws, 0 if ws is not None else bof4_token_logprobs_workspace_bytes(n, vocab, top), dev, stream)
+    _check(lib().bof4_token_logprobs(logits_at, _TYPES[logits.dtype], n, vocab, _row_stride(logits), targets_at, top,
+                                     logprob_at, entropy.data_ptr(), idx_at, top_at, stats.data_ptr(), ws.data_ptr(),
+                                     ws.numel(), _stream(stream)))
     return logprob, entropy, top_idx, top_logprob, stats
 
 
@@ -685,24 +693,21 @@ def bof4_token_logprobs_backward(logits, stats, targets=None, d_logprob=None, en
                                  out_dtype=None, stream=None):
     """The gradient by the logits, [n_rows, vocab], from bof4_token_logprobs' stats (and entropy) and the gradients of its
     logprob and entropy (float32 [n_rows]; None: that output is not used).  `out`: a tensor to fill, may be the logits."""
-    _tensor(logits, "logits", tuple(_TYPES))
+    logits_at = _tensor(logits, "logits", _TYPES)
     if logits.dim() != 2:
         raise ValueError("logits must be [n_rows, vocab]")
     n, vocab = logits.shape
-    f32 = (torch.float32,)
-    _flat(stats, "stats", f32, (n, 2), logits)
     if (targets is None) != (d_logprob is None) or (entropy is None) != (d_entropy is None):
         raise ValueError("targets come with d_logprob, the entropy with d_entropy")
+    targets_at = d_logprob_at = entropy_at = d_entropy_at = None
     if targets is not None:
-        _flat(targets, "targets", (torch.int64,), (n,), logits)
-        _flat(d_logprob, "d_logprob", f32, (n,), logits)
+        targets_at, d_logprob_at = _flat(targets, "targets", _I64, (n,)), _flat(d_logprob, "d_logprob", _F32, (n,))
     if entropy is not None:
-        _flat(entropy, "entropy", f32, (n,), logits)
-        _flat(d_entropy, "d_entropy", f32, (n,), logits)
+        entropy_at, d_entropy_at = _flat(entropy, "entropy", _F32, (n,)), _flat(d_entropy, "d_entropy", _F32, (n,))
     if out is None:
         out = torch.empty((n, vocab), dtype=out_dtype or logits.dtype, device=logits.device)
-    _tensor(out, "out", tuple(_TYPES), (n, vocab), logits)
-    _check(lib().bof4_token_logprobs_backward(_ptr(logits), _TYPES[logits.dtype], n, vocab, _row_stride(logits),
-                                              _ptr(stats), _ptr(targets), _ptr(d_logprob), _ptr(entropy), _ptr(d_entropy),
-                                              _ptr(out), _TYPES[out.dtype], _row_stride(out), _stream(stream)))
+    out_at = _tensor(out, "out", _TYPES, (n, vocab))
+    _check(lib().bof4_token_logprobs_backward(logits_at, _TYPES[logits.dtype], n, vocab, _row_stride(logits),
+                                              _flat(stats, "stats", _F32, (n, 2)), targets_at, d_logprob_at, entropy_at,
+                                              d_entropy_at, out_at, _TYPES[out.dtype], _row_stride(out), _stream(stream)))
     return out

@@ -102,7 +102,12 @@ __device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
     if constexpr (D == 4)  // mirrored in eights, then in fours
         return (uint32_t)__builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true), 0x1b, 0xf, 0xf, true);
     if constexpr (D == 8) return (uint32_t)__builtin_amdgcn_mov_dpp(x, 0x128, 0xf, 0xf, true);  // rotated by 8 of 16
-    return (uint32_t)__shfl_xor(x, D);
+    if constexpr (D == 16) {  // one copy's odd rows of 16 lanes against the other's even ones: rows 0 0 2 2 and 1 1 3 3
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return (__lane_id() & 16u) ? r[0] : r[1];
+    }
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);  // the lower half twice and the upper half twice
+    return (__lane_id() & 32u) ? r[0] : r[1];
 }
 template <int D>
 __device__ __forceinline__ uint64_t lane_xor64(uint64_t v) {
@@ -124,21 +129,25 @@ __device__ __forceinline__ uint64_t bitonic_merge(uint64_t v, uint32_t lane, boo
     if constexpr (SIZE >= 4) v = exchange<2>(v, lane, down);
     return exchange<1>(v, lane, down);
 }
-__device__ __forceinline__ uint64_t sort_descending(uint64_t v, uint32_t lane) {
+__device__ __forceinline__ uint64_t sort_ascending(uint64_t v, uint32_t lane) {
     v = bitonic_merge<2>(v, lane, (lane & 2u) == 0u);
     v = bitonic_merge<4>(v, lane, (lane & 4u) == 0u);
     v = bitonic_merge<8>(v, lane, (lane & 8u) == 0u);
     v = bitonic_merge<16>(v, lane, (lane & 16u) == 0u);
     v = bitonic_merge<32>(v, lane, (lane & 32u) == 0u);
-    return bitonic_merge<64>(v, lane, true);
+    return bitonic_merge<64>(v, lane, false);
 }
-// The 64 largest of two descending sequences, descending; `reversed`: the second one from the last lane to the first.
-__device__ __forceinline__ uint64_t merge_reversed(uint64_t list, uint64_t reversed, uint32_t lane) {
-    return bitonic_merge<64>(list > reversed ? list : reversed, lane, true);
+// The 64 largest of a descending and an ascending sequence, descending.
+__device__ __forceinline__ uint64_t merge_ascending(uint64_t list, uint64_t ascending, uint32_t lane) {
+    return bitonic_merge<64>(list > ascending ? list : ascending, lane, true);
 }
-__device__ __forceinline__ uint64_t lane_reverse64(uint64_t v, uint32_t lane) {
-    const int at = (int)(63u - lane);
-    return ((uint64_t)(uint32_t)__shfl((int)(v >> 32), at) << 32) | (uint32_t)__shfl((int)(uint32_t)v, at);
+template <int D>
+__device__ __forceinline__ uint64_t larger_of_pair(uint64_t v) {
+    const uint64_t o = lane_xor64<D>(v);
+    return v > o ? v : o;
+}
+__device__ __forceinline__ uint64_t largest_lane(uint64_t v) {  // in every lane
+    return larger_of_pair<32>(larger_of_pair<16>(larger_of_pair<8>(larger_of_pair<4>(larger_of_pair<2>(larger_of_pair<1>(v))))));
 }
 __device__ __forceinline__ uint64_t readlane64(uint64_t v, uint32_t lane) {
     return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), (int)lane) << 32) |
@@ -156,7 +165,7 @@ __device__ __forceinline__ uint64_t readlane64(uint64_t v, uint32_t lane) {
 // highest 16 bits, by bisection), so that the first tile does not bring a thousand candidates.  Every element that is
 // left out is smaller than `top` others, so the result does not depend on how the row was cut.
 //   With few rows a row is cut into n_splits parts, one per workgroup, whose records logprobs_join_kernel joins.
-constexpr uint32_t LOGPROBS_WAVES = 4, LOGPROBS_WORDS = 4;             // per workgroup; 16-byte words per lane and tile
+constexpr uint32_t LOGPROBS_WORDS = 4, LOGPROBS_JOIN_WAVES = 16; // 16-byte words per lane and tile; waves per row that joins
 constexpr uint32_t LOGPROBS_TILE = 64 * LOGPROBS_WORDS;                // words
 constexpr uint32_t LOGPROBS_MAX_SPLITS = 64, LOGPROBS_TARGET_WGS = 1024;
 constexpr uint32_t logprobs_word_elements(bool bf16) { return bf16 ? 8 : 4; }
@@ -183,15 +192,16 @@ __device__ __forceinline__ RowSums join_lanes(RowSums r) {
             __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(r.t)))};
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(64 * LOGPROBS_WAVES) void logprobs_kernel(LogprobsArgs a, uint32_t n_splits,
+template <bool BF16, uint32_t WAVES>
+__global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobsArgs a, uint32_t n_splits,
                                                                        uint32_t tiles_per_split, char* ws) {
     constexpr uint32_t PER_WORD = logprobs_word_elements(BF16), SIZE = BF16 ? 2 : 4;
     struct Shared {
-        uint4 tile[LOGPROBS_WAVES][LOGPROBS_TILE];
-        uint64_t found[LOGPROBS_WAVES][128];
-        RowSums sums[LOGPROBS_WAVES];
-        uint64_t list[LOGPROBS_WAVES][64];
+        uint4 tile[WAVES][LOGPROBS_TILE];
+        uint64_t found[WAVES][128];
+        uint64_t list[WAVES][64];
+        RowSums sums[WAVES];
+        uint32_t n_found[WAVES], has_list[WAVES];
     };
     __shared__ __attribute__((aligned(16))) Shared sh;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -253,38 +263,50 @@ __global__ __launch_bounds__(64 * LOGPROBS_WAVES) void logprobs_kernel(LogprobsA
         wave_lds_fence();
         if (64 + lane < n_found) found[lane] = rest;
         n_found = n_found > 64 ? n_found - 64 : 0;
-        list = merge_reversed(list, lane_reverse64(sort_descending(v, lane), lane), lane);
+        if (a.top == 1) {
+            const uint64_t best = largest_lane(list > v ? list : v);
+            list = lane == 0 ? best : 0;
+        } else {
+            list = merge_ascending(list, sort_ascending(v, lane), lane);
+        }
         const uint64_t last = readlane64(list, a.top - 1);
         if (last != 0) {
             last_of_list = key_logit(last);
             bound = fmaxf(bound, key_logit(last + (1ull << 32)));  // more than that: what comes later has a higher id
         }
     };
-    auto collect = [&](const Tile& t, uint32_t tile, float lane_max, uint64_t reach) {
-        float least = bound;
+    auto collect = [&](const Tile& t, const float* x, uint32_t tile, float lane_max, uint64_t reach) {
         if (__popcll(reach) > a.top) {  // what `top` lanes' maxima reach, in their highest 16 bits
             const uint32_t key = lane_max >= bound ? (uint32_t)(logit_key(lane_max, 0) >> 48) : 0u;
             uint32_t b = 0;
             for (uint32_t bit = 0x8000u; bit != 0; bit >>= 1)
                 if ((uint32_t)__popcll(__builtin_amdgcn_ballot_w64(key >= (b | bit))) >= a.top) b |= bit;
-            least = fmaxf(least, key_logit((uint64_t)b << 48));
+            bound = fmaxf(bound, key_logit((uint64_t)b << 48));
         }
+        uint32_t bits = 0;  // which of the lane's logits reach it
+#pragma unroll
+        for (uint32_t i = 0; i < LOGPROBS_WORDS * PER_WORD; ++i) bits |= x[i] >= bound ? 1u << i : 0u;
+        float least = bound;
         uint4* parked = sh.tile[wave];
 #pragma unroll
         for (uint32_t k = 0; k < LOGPROBS_WORDS; ++k) parked[64 * k + lane] = t.q[k];
         wave_lds_fence();
-        for (uint32_t i = 0; i < LOGPROBS_WORDS * PER_WORD; ++i) {
-            const uint32_t word = 64 * (i / PER_WORD) + lane;
-            const float x = load_logit<BF16>(parked, word * PER_WORD + i % PER_WORD);
-            const bool take = x >= least;
-            const uint64_t mask = __builtin_amdgcn_ballot_w64(take);
-            if (mask == 0) continue;
-            const uint32_t at = n_found + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
-            if (take) found[at] = logit_key(x, (tile * LOGPROBS_TILE + word) * PER_WORD + i % PER_WORD - off);
+        for (uint64_t mask = __builtin_amdgcn_ballot_w64(bits != 0u); mask != 0; mask = __builtin_amdgcn_ballot_w64(bits != 0u)) {
+            const uint32_t i = (uint32_t)__builtin_ctz(bits | 0x80000000u), at_word = 64 * (i / PER_WORD) + lane;
+            const float v = load_logit<BF16>(parked, at_word * PER_WORD + i % PER_WORD);
+            const uint32_t place = n_found + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+            if (bits != 0u) found[place] = logit_key(v, (tile * LOGPROBS_TILE + at_word) * PER_WORD + i % PER_WORD - off);
+            bits &= bits - 1u;
             n_found += (uint32_t)__popcll(mask);
             if (n_found >= 64) {
                 drain();
-                least = fmaxf(least, last_of_list);  // (an equal one with a lower id may follow within the tile)
+                if (last_of_list > least) {  // (an equal one with a lower id may follow within the tile)
+                    least = last_of_list;
+                    uint32_t still = 0;
+#pragma unroll
+                    for (uint32_t j = 0; j < LOGPROBS_WORDS * PER_WORD; ++j) still |= x[j] >= least ? 1u << j : 0u;
+                    bits &= still;
+                }
             }
         }
         wave_lds_fence();
@@ -324,32 +346,60 @@ __global__ __launch_bounds__(64 * LOGPROBS_WAVES) void logprobs_kernel(LogprobsA
         }
         if (a.top > 0) {
             const uint64_t reach = __builtin_amdgcn_ballot_w64(lane_max >= bound);
-            if (reach != 0) collect(t, tile, lane_max, reach);
+            if (reach != 0) collect(t, x, tile, lane_max, reach);
         }
     };
     uint32_t tile = tile0 + wave;
     if (tile < tile1) {
         Tile now = fetch(tile);
-        for (; tile < tile1; tile += LOGPROBS_WAVES) {
+        for (; tile < tile1; tile += WAVES) {
             Tile next = now;
-            if (tile + LOGPROBS_WAVES < tile1) next = fetch(tile + LOGPROBS_WAVES);
+            if (tile + WAVES < tile1) next = fetch(tile + WAVES);
             __builtin_amdgcn_sched_barrier(0);
             add(now, tile);
             now = next;
         }
     }
-    if (a.top > 0 && n_found > 0) drain();
-    // lanes, then waves, in a fixed order
-    RowSums r = {m, s0 + s1, t0 + t1};
-    r = join_lanes(r);
+    // lanes, then waves, in a fixed order; what the waves collected and did not sort yet is sorted together
+    RowSums r = join_lanes({m, s0 + s1, t0 + t1});
     if (lane == 0) sh.sums[wave] = r;
-    if (a.top > 0) sh.list[wave][lane] = list;
-    __syncthreads();
+    if (a.top > 0) {
+        const bool has_list = readlane64(list, 0) != 0;
+        if (a.top == 1) {
+            wave_lds_fence();
+            const uint64_t v = lane < n_found ? found[lane] : 0;
+            list = largest_lane(list > v ? list : v);
+            if (lane == 0) sh.list[wave][0] = list;
+        } else {
+            if (has_list) sh.list[wave][lane] = list;
+            if (lane == 0) {
+                sh.n_found[wave] = n_found;
+                sh.has_list[wave] = has_list ? 1u : 0u;
+            }
+        }
+    }
+    if (WAVES > 1) __syncthreads();
     if (wave != 0) return;
-    r = sh.sums[0];
-    for (uint32_t w = 1; w < LOGPROBS_WAVES; ++w) r = merge_sums(r, sh.sums[w]);
-    if (a.top > 0)
-        for (uint32_t w = 1; w < LOGPROBS_WAVES; ++w) list = merge_reversed(list, sh.list[w][63 - lane], lane);
+    for (uint32_t w = 1; w < WAVES; ++w) r = merge_sums(r, sh.sums[w]);
+    if (a.top == 1) {
+        for (uint32_t w = 1; w < WAVES; ++w) list = list > sh.list[w][0] ? list : sh.list[w][0];
+    } else if (a.top > 0) {
+        uint32_t total = 0, before[WAVES];
+#pragma unroll
+        for (uint32_t w = 0; w < WAVES; ++w) {
+            if (w > 0 && sh.has_list[w]) list = merge_ascending(list, sh.list[w][63 - lane], lane);
+            before[w] = total;
+            total += sh.n_found[w];
+        }
+        for (uint32_t i0 = 0; i0 < total; i0 += 64) {
+            const uint32_t i = i0 + lane;
+            uint64_t v = 0;
+#pragma unroll
+            for (uint32_t w = 0; w < WAVES; ++w)
+                if (i >= before[w] && i < (w + 1 < WAVES ? before[w + 1] : total)) v = sh.found[w][i - before[w]];
+            list = merge_ascending(list, sort_ascending(v, lane), lane);
+        }
+    }
     if (n_splits == 1) {
         finish_row<BF16>(a, row, r, list, lane);
         return;
@@ -359,29 +409,39 @@ __global__ __launch_bounds__(64 * LOGPROBS_WAVES) void logprobs_kernel(LogprobsA
     if (lane < a.top) reinterpret_cast<uint64_t*>(part + 1)[lane] = list;
 }
 
-// A row from the records of its parts, in their order: one workgroup per row, whose waves take the parts in turn.
+// A row from the records of its parts, in their order: one workgroup per row, whose waves take up to four parts each and
+// then merge their lists in pairs.
 template <bool BF16>
-__global__ __launch_bounds__(64 * LOGPROBS_WAVES) void logprobs_join_kernel(LogprobsArgs a, uint32_t n_splits, char* ws) {
-    __shared__ uint64_t lists[LOGPROBS_WAVES][64];
-    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = blockIdx.x;
+__global__ __launch_bounds__(64 * LOGPROBS_JOIN_WAVES) void logprobs_join_kernel(LogprobsArgs a, uint32_t n_splits, char* ws) {
+    static_assert(LOGPROBS_MAX_SPLITS <= 4 * LOGPROBS_JOIN_WAVES && LOGPROBS_MAX_SPLITS <= 64, "one part's sums per lane");
+    __shared__ uint64_t lists[LOGPROBS_JOIN_WAVES][64];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_waves = blockDim.x >> 6;
+    const uint32_t row = blockIdx.x;
     const uint64_t first = (uint64_t)row * n_splits;
+    RowSums r = {-INFINITY, 0.0f, 0.0f};
+    if (wave == 0 && lane < n_splits) r = logprobs_part(ws, first + lane, a.top)->r;
     uint64_t list = 0;
-    if (a.top > 0) {
-        for (uint32_t p = wave; p < n_splits; p += LOGPROBS_WAVES) {
-            const uint64_t* keys = reinterpret_cast<const uint64_t*>(logprobs_part(ws, first + p, a.top) + 1);
-            const uint32_t at = 63 - lane;
-            list = merge_reversed(list, at < a.top ? keys[at] : 0, lane);
+    if (a.top == 1) {  // (one wave)
+        list = largest_lane(lane < n_splits ? *reinterpret_cast<const uint64_t*>(logprobs_part(ws, first + lane, 1) + 1) : 0);
+    } else if (a.top > 0) {
+        uint64_t keys[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint32_t p = wave + i * n_waves, at = i == 0 ? lane : 63 - lane;
+            keys[i] = p < n_splits && at < a.top ? reinterpret_cast<const uint64_t*>(logprobs_part(ws, first + p, a.top) + 1)[at] : 0;
         }
-        lists[wave][lane] = list;
-        __syncthreads();
+        list = keys[0];
+#pragma unroll
+        for (uint32_t i = 1; i < 4; ++i)
+            if (wave + i * n_waves < n_splits) list = merge_ascending(list, keys[i], lane);
+        for (uint32_t half = n_waves / 2; half > 0; half /= 2) {
+            if (wave >= half && wave < 2 * half) lists[wave][lane] = list;
+            __syncthreads();
+            if (wave < half) list = merge_ascending(list, lists[wave + half][63 - lane], lane);
+        }
     }
     if (wave != 0) return;
-    if (a.top > 0)
-        for (uint32_t w = 1; w < LOGPROBS_WAVES; ++w) list = merge_reversed(list, lists[w][63 - lane], lane);
-    RowSums r = {-INFINITY, 0.0f, 0.0f};
-    if (lane < n_splits) r = logprobs_part(ws, first + lane, a.top)->r;
-    r = join_lanes(r);
-    finish_row<BF16>(a, row, r, list, lane);
+    finish_row<BF16>(a, row, join_lanes(r), list, lane);
 }
 
 // d x_j = g (delta_jt - p_j) - h p_j (log p_j + H), g and h the gradients of the row's log probability and entropy: read

@@ -15,18 +15,21 @@ bool valid_type(uint32_t t) { return t == BOF4_F32 || t == BOF4_BF16; }
 size_t type_bytes(uint32_t t) { return t == BOF4_BF16 ? 2 : 4; }
 constexpr uint64_t LOGPROBS_MAX_ROWS = 1ull << 23, LOGPROBS_MAX_VOCAB = 1ull << 30;  // (a launch holds fewer than 2^32 lanes)
 
-// Parts per row: with fewer rows than workgroups wanted, as many as give every wave a tile.
+// Waves and parts per row.  What a wave does at its row's end costs as much as a tile or two, so with rows enough to
+// fill the chip two waves share a row; else four, and with fewer rows than workgroups wanted a row is cut into as many
+// parts as give every wave a tile.
 struct LogprobsCut {
-    uint32_t splits, tiles_per_split;
+    uint32_t waves, splits, tiles_per_split;
 };
 LogprobsCut logprobs_cut(uint64_t n_rows, uint64_t vocab, bool bf16) {
     const uint64_t per_word = logprobs_word_elements(bf16), words = (vocab + 2 * per_word - 2) / per_word;  // wherever it begins
     const uint64_t tiles = (words + LOGPROBS_TILE - 1) / LOGPROBS_TILE;
+    const uint32_t waves = n_rows >= LOGPROBS_TARGET_WGS ? 2 : 4;
     uint64_t splits = (LOGPROBS_TARGET_WGS + n_rows - 1) / n_rows;
     if (splits > LOGPROBS_MAX_SPLITS) splits = LOGPROBS_MAX_SPLITS;
     uint64_t per = (tiles + splits - 1) / splits;
-    if (per < LOGPROBS_WAVES) per = LOGPROBS_WAVES;
-    return {(uint32_t)((tiles + per - 1) / per), (uint32_t)per};
+    if (per < waves) per = waves;
+    return {waves, (uint32_t)((tiles + per - 1) / per), (uint32_t)per};
 }
 }  // namespace
 
@@ -63,19 +66,24 @@ int bof4_token_logprobs(const void* logits_dev, uint32_t logits_type, uint64_t n
                             logprob_dev, entropy_dev, top_logprob_dev, stats_dev, top_idx_dev};
     const bool bf16 = logits_type == BOF4_BF16;
     const LogprobsCut cut = logprobs_cut(n_rows, vocab, bf16);
-    const dim3 grid(a.n_rows * cut.splits), threads(64 * LOGPROBS_WAVES);
     timing_begin(s);
+#define BOF4_LAUNCH_LOGPROBS(BF16_, WAVES_)                                                                                   \
+    hipLaunchKernelGGL((logprobs_kernel<BF16_, WAVES_>), dim3(a.n_rows * cut.splits), dim3(64 * WAVES_), 0, s, a, cut.splits, \
+                       cut.tiles_per_split, (char*)ws_dev);
     if (bf16) {
-        hipLaunchKernelGGL((logprobs_kernel<true>), grid, threads, 0, s, a, cut.splits, cut.tiles_per_split, (char*)ws_dev);
+        if (cut.waves == 2) { BOF4_LAUNCH_LOGPROBS(true, 2) } else { BOF4_LAUNCH_LOGPROBS(true, 4) }
     } else {
-        hipLaunchKernelGGL((logprobs_kernel<false>), grid, threads, 0, s, a, cut.splits, cut.tiles_per_split, (char*)ws_dev);
+        if (cut.waves == 2) { BOF4_LAUNCH_LOGPROBS(false, 2) } else { BOF4_LAUNCH_LOGPROBS(false, 4) }
     }
+#undef BOF4_LAUNCH_LOGPROBS
     timing_end(s);
     if (cut.splits > 1) {
+        uint32_t waves = 1;  // one of two to four parts' lists each; one where there are no lists of more than one
+        while (top > 1 && waves < LOGPROBS_JOIN_WAVES && 2 * waves < cut.splits) waves *= 2;
         if (bf16) {
-            hipLaunchKernelGGL((logprobs_join_kernel<true>), dim3(a.n_rows), threads, 0, s, a, cut.splits, (char*)ws_dev);
+            hipLaunchKernelGGL((logprobs_join_kernel<true>), dim3(a.n_rows), dim3(64 * waves), 0, s, a, cut.splits, (char*)ws_dev);
         } else {
-            hipLaunchKernelGGL((logprobs_join_kernel<false>), dim3(a.n_rows), threads, 0, s, a, cut.splits, (char*)ws_dev);
+            hipLaunchKernelGGL((logprobs_join_kernel<false>), dim3(a.n_rows), dim3(64 * waves), 0, s, a, cut.splits, (char*)ws_dev);
         }
     }
     HIP_TRY(hipGetLastError());
