@@ -375,6 +375,69 @@ int bof4_gemm_outlier_table(const uint8_t* codes_dev, const uint16_t* scales_dev
 size_t bof4_gemm_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t n_tokens);
 
 /*
+ * A linear layer around the products with a quantised matrix, in one call and without the product on its way through memory:
+ *     z = x W^T + bias,   y = act(z) * mul + residual
+ * with W and its list as bof4_gemv (bof4_gemv_linear: one token to a few) or bof4_gemm (bof4_gemm_linear: 8 or more) takes
+ * them, and the sums as those make them (their order and errors are stated there).  Everything behind the sums is binary32; each
+ * tensor written is rounded once.  The gate of a gated layer is mul: with u = x Wu^T, silu(x Wg^T) * u.
+ */
+#define BOF4_ACT_NONE 0u
+#define BOF4_ACT_RELU 1u
+#define BOF4_ACT_GELU 2u      /* z (1 + erf(z / sqrt 2)) / 2 */
+#define BOF4_ACT_GELU_TANH 3u /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+#define BOF4_ACT_SILU 4u      /* z / (1 + exp(-z)) */
+/* What belongs to a layer besides the matrix (host struct, read during the call).  Types are BOF4_F32 or BOF4_BF16; ld_* are
+ * elements from one token to the next (>= rows); every pointer has its element's alignment (four elements' alignment of all
+ * pointers and row strides saves time). */
+typedef struct {
+    uint32_t act;                                               /* BOF4_ACT_*                                        */
+    uint32_t bias_type, mul_type, residual_type, y_type, pre_type;
+    const void* bias_dev;                                       /* rows, or NULL                                      */
+    const void* mul_dev;                                        /* n_tokens x rows, or NULL                           */
+    const void* residual_dev;                                   /* n_tokens x rows, or NULL                           */
+    void* y_dev;                                                /* n_tokens x rows; may be mul or the residual itself */
+    void* pre_dev;                                              /* z for the backward pass, n_tokens x rows, or NULL  */
+    uint64_t ld_mul, ld_residual, ld_y, ld_pre;
+} bof4_layer;
+/* bof4_gemv's arguments with the layer in the place of y, and its limits but 2^30 rows.  Only enqueues. */
+int bof4_gemv_linear(const uint8_t* codes_dev, const uint16_t* scales_dev, uint64_t rows, uint64_t cols, uint32_t block,
+                     const double* cb_host, const void* table_dev, uint64_t n_outliers, const void* x_dev, uint32_t n_tokens,
+                     const bof4_layer* layer, void* stream);
+/* bof4_gemm's arguments with the layer in the place of y, and its limits but 2^30 rows; the workspace is
+ * bof4_gemm_linear_workspace_bytes(rows, cols, n_tokens), which never falls as n_tokens rises.  Only enqueues. */
+int bof4_gemm_linear(const void* packed_dev, uint64_t rows, uint64_t cols, const double* cb_host, const void* table_dev,
+                     uint64_t n_outliers, const void* x_dev, uint32_t n_tokens, const bof4_layer* layer, void* ws_dev,
+                     size_t ws_bytes, void* stream);
+size_t bof4_gemm_linear_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t n_tokens);
+
+/*
+ * The gradients of that layer by what is trained around a frozen quantised matrix (fine-tuning through 4-bit weights):
+ *     dz = dy * mul * act'(pre),   dx = dz W^,   dmul = dy * act(pre),   dbias = sum over the tokens of dz
+ * (and the residual's gradient is dy itself), W^ the bfloat16 matrix of bof4_gemm from its packed copy and table.  dz is
+ * rounded to bfloat16 for the matrix cores (where there is neither act nor mul and dy is bfloat16 it is dy, exactly); the sums
+ * of dx are binary32 over the rows in a fixed order, within (rows + 64) * 2^-24 * sum_r |dz W^| of the exact ones; dbias sums dz
+ * before that rounding.  Equal calls give equal bits.
+ */
+typedef struct {
+    uint32_t act;                                               /* BOF4_ACT_*, as in the forward call                  */
+    uint32_t dy_type, pre_type, mul_type, dmul_type, dx_type;
+    const void* dy_dev;                                         /* n_tokens x rows                                      */
+    const void* pre_dev;                                        /* n_tokens x rows; NULL if neither act nor dmul needs it */
+    const void* mul_dev;                                        /* n_tokens x rows, or NULL: no factor                  */
+    void* dmul_dev;                                             /* n_tokens x rows, or NULL; may be dy, pre or mul itself */
+    float* dbias_dev;                                           /* rows, or NULL                                        */
+    void* dx_dev;                                               /* n_tokens x cols                                      */
+    uint64_t ld_dy, ld_pre, ld_mul, ld_dmul, ld_dx;
+} bof4_layer_gradient;
+/* ws_dev: bof4_gemm_linear_backward_workspace_bytes(rows, cols, n_tokens) bytes (256-byte aligned), which never falls as
+ * n_tokens rises: dz, partial sums, and the decoded matrix in slabs of up to 256 MiB.  Limits: rows <= 2^18, cols <= 32768 and a
+ * multiple of 32, n_tokens <= 65536.  Only enqueues. */
+int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t cols, const double* cb_host, const void* table_dev,
+                              uint64_t n_outliers, uint32_t n_tokens, const bof4_layer_gradient* gradient, void* ws_dev,
+                              size_t ws_bytes, void* stream);
+size_t bof4_gemm_linear_backward_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t n_tokens);
+
+/*
  * Log probabilities of given tokens from a model's logits, with the entropy and the largest alternatives of every row:
  * what the perplexity of section 5 is the exponential of, and what a model is trained and sampled by.  For row i of
  * n_rows, with p = softmax of its `vocab` logits:

@@ -20,7 +20,9 @@ EXPORTS = ("bof4_workspace_bytes", "bof4_opq_threshold", "bof4_thresholds", "bof
            "bof4_quant_error", "bof4_gemv", "bof4_gemv_outlier_table",
            "bof4_gemv_outlier_table_bytes", "bof4_gemm", "bof4_gemm_pack", "bof4_gemm_packed_bytes",
            "bof4_gemm_outlier_table", "bof4_gemm_workspace_bytes",
-           "bof4_token_logprobs", "bof4_token_logprobs_workspace_bytes", "bof4_token_logprobs_backward",
+           "bof4_gemv_linear", "bof4_gemm_linear", "bof4_gemm_linear_workspace_bytes", "bof4_gemm_linear_backward",
+           "bof4_gemm_linear_backward_workspace_bytes", "bof4_token_logprobs", "bof4_token_logprobs_workspace_bytes",
+           "bof4_token_logprobs_backward",
            "bof4_theory_centroids", "bof4_theory_workspace_bytes", "bof4_time_next_call", "bof4_last_error",
            "bof4_last_hip_error")
 
@@ -58,6 +60,20 @@ class MaeStats(ctypes.Structure):
         return {"median": np.array(self.median[:], dtype=np.float64), "den": np.array(self.den[:], dtype=np.float64),
                 "cnt": np.array(self.cnt[:], dtype=np.uint64), "sae": float(self.sae),
                 "n_used": int(self.n_used), "n_outliers": int(self.n_outliers)}
+
+
+class Layer(ctypes.Structure):
+    """bof4_layer of include/bof4.h."""
+    _fields_ = ([("act", ctypes.c_uint32)] + [(k + "_type", ctypes.c_uint32) for k in ("bias", "mul", "residual", "y", "pre")]
+                + [(k + "_dev", ctypes.c_void_p) for k in ("bias", "mul", "residual", "y", "pre")]
+                + [("ld_" + k, ctypes.c_uint64) for k in ("mul", "residual", "y", "pre")])
+
+
+class LayerGradient(ctypes.Structure):
+    """bof4_layer_gradient of include/bof4.h."""
+    _fields_ = ([("act", ctypes.c_uint32)] + [(k + "_type", ctypes.c_uint32) for k in ("dy", "pre", "mul", "dmul", "dx")]
+                + [(k + "_dev", ctypes.c_void_p) for k in ("dy", "pre", "mul", "dmul", "dbias", "dx")]
+                + [("ld_" + k, ctypes.c_uint64) for k in ("dy", "pre", "mul", "dmul", "dx")])
 
 
 _lib = None
@@ -136,6 +152,15 @@ def lib():
         L.bof4_gemm_workspace_bytes.restype = ctypes.c_size_t
         L.bof4_gemm_workspace_bytes.argtypes = [ctypes.c_uint64, ctypes.c_uint64, ctypes.c_uint32]
         u32, u64, size = ctypes.c_uint32, ctypes.c_uint64, ctypes.c_size_t
+        L.bof4_gemv_linear.restype = ctypes.c_int
+        L.bof4_gemv_linear.argtypes = [vp, vp, u64, u64, u32, f64p, vp, u64, vp, u32, ctypes.POINTER(Layer), vp]
+        L.bof4_gemm_linear.restype = ctypes.c_int
+        L.bof4_gemm_linear.argtypes = [vp, u64, u64, f64p, vp, u64, vp, u32, ctypes.POINTER(Layer), vp, size, vp]
+        L.bof4_gemm_linear_backward.restype = ctypes.c_int
+        L.bof4_gemm_linear_backward.argtypes = [vp, u64, u64, f64p, vp, u64, u32, ctypes.POINTER(LayerGradient), vp, size, vp]
+        for name in ("bof4_gemm_linear_workspace_bytes", "bof4_gemm_linear_backward_workspace_bytes"):
+            getattr(L, name).restype = size
+            getattr(L, name).argtypes = [u64, u64, u32]
         L.bof4_token_logprobs.restype = ctypes.c_int
         L.bof4_token_logprobs.argtypes = [vp, u32, u64, u64, u64, vp, u32, vp, vp, vp, vp, vp, vp, size, vp]
         L.bof4_token_logprobs_workspace_bytes.restype = size
@@ -655,6 +680,119 @@ def _scratch(ws, nbytes, device, stream):
     if stream is not None:
         ws.record_stream(stream)
     return ws
+
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}  # BOF4_ACT_*
+
+
+def _activation(act):
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}")
+    return ACTIVATIONS[act]
+
+
+def _layer_input(x, cols):
+    x2 = x if x.dim() == 2 else x[None, :]
+    if x2.dtype != torch.bfloat16 or x2.shape[1] != cols or not x2.is_contiguous():
+        raise ValueError("x must be a contiguous bfloat16 tensor of [n_tokens, cols]")
+    _tensor(x2, "x", _TYPES)
+    return x2
+
+
+def _rows_of(record, key, t, shape):
+    """Address, type and row stride of a tensor of tokens x rows (or None) into the record's fields."""
+    if t is not None:
+        setattr(record, key + "_dev", _tensor(t, key, _TYPES, shape))
+        setattr(record, key + "_type", _TYPES[t.dtype])
+        setattr(record, "ld_" + key, _row_stride(t))
+
+
+def _layer(n_tokens, rows, bias, act, mul, residual, pre, out):
+    layer, shape = Layer(), (n_tokens, rows)
+    layer.act = _activation(act)
+    if bias is not None:
+        layer.bias_dev, layer.bias_type = _flat(bias, "bias", _TYPES, (rows,)), _TYPES[bias.dtype]
+    _rows_of(layer, "mul", mul, shape)
+    _rows_of(layer, "residual", residual, shape)
+    _rows_of(layer, "pre", pre, shape)
+    _rows_of(layer, "y", out, shape)
+    return layer
+
+
+def bof4_gemv_linear(codes, scales, rows, cols, block, cb, x, table=None, n_outliers=0, bias=None, act="none", mul=None,
+                     residual=None, pre=None, out=None, out_dtype=torch.bfloat16, stream=None):
+    """y = act(x W~^T + bias) * mul + residual for one token to a few; matrix, x, table as for bof4_gemv.  bias [rows], mul,
+    residual, pre, out [n_tokens, rows] (rows of any stride): bfloat16 or float32 each.  act: a key of ACTIVATIONS.  `pre`: a
+    tensor that receives x W~^T + bias; `out`: the result's, may be mul or the residual (else of `out_dtype`)."""
+    cb, cbp = _cb(cb)
+    x2 = _layer_input(x, cols)
+    n_tokens, k = int(x2.shape[0]), int(n_outliers)
+    if k and table is None:
+        raise ValueError("outliers need their table (bof4_gemv_outlier_table)")
+    if out is None:
+        out = torch.empty((n_tokens, rows), dtype=out_dtype, device=x.device)
+    layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out)
+    _check(lib().bof4_gemv_linear(codes.data_ptr(), scales.data_ptr(), rows, cols, block, cbp, table.data_ptr() if k else None, k,
+                                  x2.data_ptr(), n_tokens, layer, _stream(stream)))
+    return out
+
+
+def bof4_gemm_linear_workspace_bytes(rows, cols, n_tokens):
+    return int(lib().bof4_gemm_linear_workspace_bytes(rows, cols, n_tokens))
+
+
+def bof4_gemm_linear(packed, rows, cols, cb, x, table=None, n_outliers=0, bias=None, act="none", mul=None, residual=None,
+                     pre=None, out=None, out_dtype=torch.bfloat16, ws=None, stream=None):
+    """y = act(x W^^T + bias) * mul + residual for many tokens; matrix, x, table as for bof4_gemm, the rest as for
+    bof4_gemv_linear; `ws`: optional uint8 device tensor of bof4_gemm_linear_workspace_bytes(...) bytes."""
+    cb, cbp = _cb(cb)
+    x2 = _layer_input(x, cols)
+    if packed.numel() < bof4_gemm_packed_bytes(rows, cols):
+        raise ValueError("packed matrix too small for rows x cols (bof4_gemm_pack)")
+    n_tokens, k = int(x2.shape[0]), int(n_outliers)
+    if k and table is None:
+        raise ValueError("outliers need their table (bof4_gemm_outlier_table)")
+    if out is None:
+        out = torch.empty((n_tokens, rows), dtype=out_dtype, device=x.device)
+    layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out)
+    ws = _scratch(ws, 0 if ws is not None else bof4_gemm_linear_workspace_bytes(rows, cols, n_tokens), x.device, stream)
+    _check(lib().bof4_gemm_linear(packed.data_ptr(), rows, cols, cbp, table.data_ptr() if k else None, k, x2.data_ptr(),
+                                  n_tokens, layer, ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out
+
+
+def bof4_gemm_linear_backward_workspace_bytes(rows, cols, n_tokens):
+    return int(lib().bof4_gemm_linear_backward_workspace_bytes(rows, cols, n_tokens))
+
+
+def bof4_gemm_linear_backward(packed, rows, cols, cb, dy, table=None, n_outliers=0, act="none", pre=None, mul=None, dmul=None,
+                              dbias=None, out=None, out_dtype=torch.bfloat16, ws=None, stream=None):
+    """The gradients of bof4_gemm_linear: returns dx [n_tokens, cols] (`out`, else of `out_dtype`) from dy [n_tokens, rows] and,
+    as the forward call had them, act, pre (what it wrote) and mul.  `dmul` [n_tokens, rows] and `dbias` float32 [rows]: tensors
+    that receive those gradients (the residual's is dy)."""
+    cb, cbp = _cb(cb)
+    if dy.dim() != 2 or dy.shape[1] != rows:
+        raise ValueError("dy must be [n_tokens, rows]")
+    if packed.numel() < bof4_gemm_packed_bytes(rows, cols):
+        raise ValueError("packed matrix too small for rows x cols (bof4_gemm_pack)")
+    n_tokens, k = int(dy.shape[0]), int(n_outliers)
+    if k and table is None:
+        raise ValueError("outliers need their table (bof4_gemm_outlier_table)")
+    if out is None:
+        out = torch.empty((n_tokens, cols), dtype=out_dtype, device=dy.device)
+    g, shape = LayerGradient(), (n_tokens, rows)
+    g.act = _activation(act)
+    _rows_of(g, "dy", dy, shape)
+    _rows_of(g, "pre", pre, shape)
+    _rows_of(g, "mul", mul, shape)
+    _rows_of(g, "dmul", dmul, shape)
+    _rows_of(g, "dx", out, (n_tokens, cols))
+    if dbias is not None:
+        g.dbias_dev = _flat(dbias, "dbias", _F32, (rows,))
+    ws = _scratch(ws, 0 if ws is not None else bof4_gemm_linear_backward_workspace_bytes(rows, cols, n_tokens), dy.device, stream)
+    _check(lib().bof4_gemm_linear_backward(packed.data_ptr(), rows, cols, cbp, table.data_ptr() if k else None, k, n_tokens, g,
+                                           ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out
 
 
 def bof4_token_logprobs_workspace_bytes(n_rows, vocab, top=0):

@@ -50,7 +50,7 @@ __device__ __forceinline__ uint32_t gemm_pack_bf16(float lo, float hi) {
 // tile, columns 32 (lane / 32) .. + 31 of the chunk), then one binary16 constant per lane (that of the lane's 32
 // columns).  Rows past the matrix and columns past its width hold code 0 and constant 0: they add nothing.
 constexpr uint32_t GEMM_TILE_BYTES = 64 * 16 + 64 * 2;
-__global__ __launch_bounds__(256) void gemm_pack_weights_kernel(const uint4* __restrict__ codes,
+static __global__ __launch_bounds__(256) void gemm_pack_weights_kernel(const uint4* __restrict__ codes,
                                                                 const uint16_t* __restrict__ scales, uint32_t rows,
                                                                 uint32_t cols, uint32_t log2_block, uint32_t n_chunks,
                                                                 uint64_t n_tiles, char* __restrict__ packed) {
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256) void gemm_pack_weights_kernel(const uint4* __r
 // x in the order the products read it, made once per call: for every tile of 32 tokens, chunk of 64 columns and
 // product j one 16-byte word per lane (token = lane % 32 of the tile, columns 32 (lane / 32) + 8 j .. + 7 of the
 // chunk), so that a wave's load is 1 KiB of consecutive memory; zeros past the last token and the last column.
-__global__ __launch_bounds__(256) void gemm_pack_x_kernel(const uint16_t* __restrict__ x, uint32_t n_tokens,
+static __global__ __launch_bounds__(256) void gemm_pack_x_kernel(const uint16_t* __restrict__ x, uint32_t n_tokens,
                                                           uint32_t cols, uint32_t n_chunks, uint32_t n_pad,
                                                           uint4* __restrict__ xp) {
     const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
@@ -126,7 +126,7 @@ static_assert(GEMM_MAX_COLS == GEMV_MAX_STRIPS * GEMV_STRIP, "both products take
 // position of its row tile is below 2^20, so rows and columns come from a 32-bit division: 500 x 28672 with 0.7 %
 // outliers took 21 us with 64-bit divisions and 256 lanes.
 constexpr uint32_t GEMM_LIST_WGS = 1u << 20;
-__global__ __launch_bounds__(1024) void gemm_list_kernel(const int64_t* __restrict__ out_idx,
+static __global__ __launch_bounds__(1024) void gemm_list_kernel(const int64_t* __restrict__ out_idx,
                                                          const uint16_t* __restrict__ out_val, uint32_t n_out,
                                                          uint64_t rows, uint32_t cols, uint32_t row_tiles,
                                                          GemmListGeometry lg, uint32_t* __restrict__ ptr,
@@ -209,12 +209,12 @@ __device__ __forceinline__ void gemm_carry(gemm_f32x16& sum, gemm_f32x16& acc, i
 // The packed matrix holds a multiple of GEMM_MAX_R row tiles.
 template <int R, int NT>
 constexpr bool GEMM_CARRY = R == 1 || NT == 2;
-template <int R, int NT, bool OUTLIERS, bool X_IN_PLACE>
+template <int R, int NT, bool OUTLIERS, bool X_IN_PLACE, class Out>
 __global__ __launch_bounds__(64 * GEMM_MAX_WAVES, X_IN_PLACE ? 4 : 2) void gemm_kernel(
     const char* __restrict__ packed, uint32_t rows, uint32_t cols, CodebookArgs cb, const uint32_t* __restrict__ list_ptr,
     const uint32_t* __restrict__ entries, uint32_t n_out, GemmListGeometry lg, uint32_t row_tiles,
     const uint4* __restrict__ xp, const uint16_t* __restrict__ x, uint32_t tile0, uint32_t n_tokens, uint32_t flush,
-    uint32_t n_runs, float* __restrict__ dst) {
+    uint32_t n_runs, Out dst) {
     static_assert(!X_IN_PLACE || NT == 1, "one tile of tokens");
     constexpr uint32_t N_RED = R * NT > 1 && !(OUTLIERS && R * NT > 6) ? 2 : 1;  // (the largest one would spill)
     struct Shared {
@@ -356,7 +356,8 @@ __global__ __launch_bounds__(64 * GEMM_MAX_WAVES, X_IN_PLACE ? 4 : 2) void gemm_
     // half of the chunks (or all of them) the result, for the first half the record that the second half starts from.
     // Accumulator i of lane l: row 8 (i / 4) + 4 (l / 32) + i % 4 of the tile, token l % 32; a thread adds two
     // neighbouring rows of one token.
-    float* out = dst + (uint64_t)blockIdx.y * n_tokens * rows;
+    const bool as_sums = !Out::LAYER || gridDim.y > 1;
+    float* out = dst.part(blockIdx.y, n_tokens, rows);
     auto reduce = [&](const uint32_t run, const bool last_run) __attribute__((always_inline)) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -401,6 +402,13 @@ __global__ __launch_bounds__(64 * GEMM_MAX_WAVES, X_IN_PLACE ? 4 : 2) void gemm_
                     }
                     const uint32_t l = (p >> 1) & 63, row = r0 + 8 * (p >> 7) + 4 * (l >> 5) + 2 * (p & 1), n = 32 * t + (l & 31);
                     if (n >= n_tokens) continue;
+                    if constexpr (Out::LAYER) {
+                        if (!as_sums) {
+                            const float sums[2] = {(float)s0, (float)s1};
+                            if (row < rows) dst.template store<2>(n, row, rows, sums);
+                            continue;
+                        }
+                    }
                     float* o = out + (uint64_t)n * rows + row;
                     if (row + 1 < rows) {
                         const gemm_f32x2_any v = {(float)s0, (float)s1};
@@ -475,6 +483,37 @@ __global__ __launch_bounds__(64 * GEMM_MAX_WAVES, X_IN_PLACE ? 4 : 2) void gemm_
     }
 }
 
+// A layer's result of the 2 x 2 tiles of a wave of the 256 x 128 tile: each is turned in LDS, so that a lane holds four
+// neighbouring rows of one token and eight lanes write 64 bytes (or 128) of it; one copy of the layer's code in a loop,
+// where 64 sums in registers would need as many.
+constexpr uint32_t GEMM_STAGE_LD = 40;  // floats from one token to the next: the two halves of a wave meet in no bank
+template <class Out>
+__device__ __forceinline__ void gemm_store_tiles(const Out& dst, void* lds, uint32_t wave, uint32_t lane, gemm_f32x16 (&sum)[2][2],
+                                                 gemm_f32x16 (&acc)[2][2], uint32_t row0, uint32_t rows, uint32_t token0,
+                                                 uint32_t n_tokens) {
+    float* stage = reinterpret_cast<float*>(lds) + wave * (GEMM_TOKENS * GEMM_STAGE_LD);
+    __syncthreads();  // the operands that stood here have been read
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            wave_lds_fence();
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                stage[(8 * (i >> 2) + 4 * (lane >> 5) + (i & 3)) * GEMM_STAGE_LD + (lane & 31)] = sum[r][t][i] + acc[r][t][i];
+            wave_lds_fence();
+            const uint32_t row = row0 + r * GEMM_ROWS + 4 * (lane & 7);
+            for (uint32_t k = lane >> 3; k < GEMM_TOKENS; k += 8) {
+                const uint32_t token = token0 + t * GEMM_TOKENS + k;
+                if (row >= rows || token >= n_tokens) continue;
+                const float4 v = *reinterpret_cast<const float4*>(stage + k * GEMM_STAGE_LD + 4 * (lane & 7));
+                const float sums[4] = {v.x, v.y, v.z, v.w};
+                dst.template store<4>(token, row, rows, sums);
+            }
+        }
+    }
+}
+
 // Many tokens: the same product with a tile of 256 rows x 128 tokens per workgroup of eight waves.  gemm_kernel reads
 // all of x once per 64 rows (0.8 GB per 128 tokens through a Llama-7B-shaped block, and it ran at the rate at which the
 // caches deliver that); here the decoded weights and x are shared through LDS, so x is read once per 256 rows and a
@@ -496,12 +535,12 @@ __global__ __launch_bounds__(64 * GEMM_MAX_WAVES, X_IN_PLACE ? 4 : 2) void gemm_
 // TFLOP/s), 4096 x 4096 257 -> 100; with one 22016 x 4096 1087 -> 589, 57344 x 8192 3503 -> 2590, 4096 x 4096 305 -> 122.
 // The weights are the second operand here: accumulator i of lane l is token 8 (i / 4) + 4 (l / 32) + i % 4 and row
 // l % 32, so that a store of a wave writes two runs of 128 bytes.
-template <bool OUTLIERS, bool CARRY>
+template <bool OUTLIERS, bool CARRY, class Out>
 __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_wide_kernel(
     const char* __restrict__ packed, uint32_t rows, uint32_t cols, CodebookArgs cb, const uint32_t* __restrict__ list_ptr,
     const uint32_t* __restrict__ entries, uint32_t n_out, GemmListGeometry lg, uint32_t row_tiles, uint32_t packed_tiles,
     const uint4* __restrict__ xp, uint32_t tok_tiles, uint32_t tok_groups, uint32_t per_split, uint32_t flush,
-    uint32_t n_tokens, float* __restrict__ y, float* __restrict__ parts) {
+    uint32_t n_tokens, uint32_t n_parts, Out dst) {
     struct Shared {
         float tab[16];
         uint16_t unused[GEMM_WIDE_WAVES][64];  // where lanes without an entry write
@@ -707,8 +746,15 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_wide_kernel(
         if (s + 1 < n_steps) step(s + 1, 1, o3, o4.q.x);
     }
 
-    // the first part goes to the result itself, where gemm_sum_kernel adds the others to it
-    float* out = part == 0 ? y : parts + (uint64_t)(part - 1) * n_tokens * rows;
+    if constexpr (Out::LAYER) {
+        if (n_parts == 1) {
+            gemm_store_tiles(dst, &sh.a[0][0][0], wave, lane, sum, acc, (rg * GEMM_WIDE_WAVES + wr) * GEMM_ROWS, rows,
+                             (tg * GEMM_WIDE_TOK_TILES + wt) * GEMM_TOKENS, n_tokens);
+            return;
+        }
+    }
+    // the first part of a plain product goes to the result itself, where gemm_sum_kernel adds the others to it
+    float* out = dst.part(part, n_tokens, rows);
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const uint32_t row = (rg * GEMM_WIDE_WAVES + wr + r) * GEMM_ROWS + (lane & 31);
@@ -822,11 +868,11 @@ __global__ __launch_bounds__(64 * GEMM_DECODE_WAVES) void gemm_decode_kernel(
 // after four reads; the waves' priority raised for the products 4 to 8 % slower; the tiles' sums carried in turns no difference.
 //   2000 tokens with a list, gemm_wide_kernel -> decoding and this: 4096 x 4096 127 -> 102 us, 12288 x 4096 353 -> 252, 22016 x
 // 4096 649 -> 482, 8192 x 28672 1305 -> 1042.
-template <bool CARRY>
+template <bool CARRY, class Out>
 __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
     const uint4* __restrict__ decoded, uint32_t first_row, uint32_t n_rt, uint32_t rows, uint32_t n_chunks,
     const uint4* __restrict__ xp, uint32_t tok_tiles, uint32_t tok_groups, uint32_t per_split, uint32_t flush,
-    uint32_t n_tokens, float* __restrict__ y, float* __restrict__ parts) {
+    uint32_t n_tokens, uint32_t n_parts, Out dst) {
     struct Shared {
         uint4 a[3][GEMM_WIDE_WAVES][GEMM_TILE_WORDS];
         uint4 b[3][GEMM_WIDE_TOK_TILES][GEMM_TILE_WORDS];
@@ -964,8 +1010,16 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
             }
         }
     }
-    // the first part goes to the result itself, where gemm_sum_kernel adds the others to it
-    float* out = part == 0 ? y : parts + (uint64_t)(part - 1) * n_tokens * rows;
+    if constexpr (Out::LAYER) {
+        if (n_parts == 1) {
+            gemm_store_tiles(dst, &sh.a[0][0][0], wave, lane, sum, acc, first_row + (rg * GEMM_WIDE_WAVES + wr) * GEMM_ROWS,
+                             min(rows, first_row + n_rt * GEMM_ROWS),
+                             (tg * GEMM_WIDE_TOK_TILES + wt) * GEMM_TOKENS, n_tokens);
+            return;
+        }
+    }
+    // the first part of a plain product goes to the result itself, where gemm_sum_kernel adds the others to it
+    float* out = dst.part(part, n_tokens, rows);
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const uint32_t rt = rg * GEMM_WIDE_WAVES + wr + r, row = first_row + rt * GEMM_ROWS + (lane & 31);
@@ -982,13 +1036,36 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
 }
 
 // y = the partial results in order (count elements each): the first, which may stand in y itself, and n_more others.
-__global__ __launch_bounds__(256) void gemm_sum_kernel(const float* first, const float* __restrict__ more, uint32_t n_more,
+static __global__ __launch_bounds__(256) void gemm_sum_kernel(const float* first, const float* __restrict__ more, uint32_t n_more,
                                                        uint64_t count, float* y) {
     const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
     if (idx >= count) return;
     double s = first[idx];
     for (uint32_t k = 0; k < n_more; ++k) s += more[k * count + idx];
     y[idx] = (float)s;
+}
+
+
+// A layer's result from the partial sums in order (n_parts of n_tokens x rows each).  A workgroup takes 1024 rows, four to a
+// lane, of the tokens blockIdx.y, + gridDim.y, ...
+template <class Out>
+__global__ __launch_bounds__(256) void gemm_sum_layer_kernel(uint32_t n_parts, uint32_t n_tokens, uint32_t rows, Out dst) {
+    const uint32_t row = (blockIdx.x * 256 + threadIdx.x) * 4;
+    if (row >= rows) return;
+    const uint64_t count = (uint64_t)n_tokens * rows;
+    for (uint32_t token = blockIdx.y; token < n_tokens; token += gridDim.y) {
+        const float* p = dst.parts + (uint64_t)token * rows + row;
+        const bool whole = row + 4 <= rows && (rows & 3u) == 0u;
+        double s[4] = {0.0, 0.0, 0.0, 0.0};
+        for (uint32_t k = 0; k < n_parts; ++k, p += count) {
+            float v[4];
+            load_row<4>(p, 0, false, whole, rows - row, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] += v[i];
+        }
+        const float sums[4] = {(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
+        dst.template store<4>(token, row, rows, sums);
+    }
 }
 
 }  // namespace bof4

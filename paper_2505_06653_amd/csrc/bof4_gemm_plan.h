@@ -228,10 +228,16 @@ inline GemmDecodedPlan gemm_decoded_choice(uint64_t rows, uint64_t cols, uint64_
 // gemm_kernel's lie behind `part`; the wide kernel's - all but the first part's, which goes to y - behind `wide_part`.
 // `total` is what a call cannot do without and what gemm_kernel takes; it holds room for a second copy of x that only the
 // wide kernel's partial results use (x transposed once stood there: buffers of that size are in use).
+// A layer (`layer`: a product whose sums go through its bias, activation and so on before they are stored) has no place in
+// y for the first part: all of them lie behind `wide_part` where there are several.
+inline uint64_t gemm_wide_parts(uint64_t split, bool layer) { return layer && split > 1 ? split : split - 1; }
 struct GemmWsLayout {
     size_t xp, part, wide_part, total;
-    size_t decoded(uint64_t split, uint64_t n_tokens, uint64_t rows) const {  // behind the partial results of the 256 x 128 tile
-        return align_up(wide_part + (split - 1) * n_tokens * rows * 4, 256);
+    size_t wide(uint64_t split, uint64_t n_tokens, uint64_t rows, bool layer) const {  // the end of the 256 x 128 tile's parts
+        return wide_part + gemm_wide_parts(split, layer) * n_tokens * rows * 4;
+    }
+    size_t decoded(uint64_t split, uint64_t n_tokens, uint64_t rows, bool layer = false) const {  // behind them
+        return align_up(wide(split, n_tokens, rows, layer), 256);
     }
 };
 inline GemmWsLayout gemm_ws_layout(uint64_t rows, uint64_t cols, uint64_t n_tokens) {
@@ -250,7 +256,7 @@ inline GemmWsLayout gemm_ws_layout(uint64_t rows, uint64_t cols, uint64_t n_toke
 // tokens).  Splits and slabs are the same for all token tiles of a group, so the most tokens of a group for which a kernel is
 // chosen need the most: 8192 x 28672 at 2000 / 65536 tokens 29 us / 0.37 ms, 4096 x 4096 15 us / 0.18 ms (45 / 1500 and 30 / 1000
 // where every token tile is asked about).
-inline size_t gemm_ws_bytes(uint64_t rows, uint64_t cols, uint64_t n_tokens) {
+inline size_t gemm_ws_bytes(uint64_t rows, uint64_t cols, uint64_t n_tokens, bool layer = false) {
     size_t need = gemm_ws_layout(rows, cols, n_tokens).total;
     const uint64_t most = n_tokens < GEMM_MAX_TOKENS ? n_tokens : GEMM_MAX_TOKENS;
     const uint64_t all_tiles = (most + GEMM_TOKENS - 1) / GEMM_TOKENS;
@@ -262,14 +268,14 @@ inline size_t gemm_ws_bytes(uint64_t rows, uint64_t cols, uint64_t n_tokens) {
             for (const bool list : {true, false}) {  // (which kernel is chosen depends on it, neither way the other's superset)
                 const GemmWideSplit W = gemm_wide_choice(rows, cols, tiles, list);
                 if (W.split > 0 && !has_wide) {
-                    const size_t bytes = gemm_ws_layout(rows, cols, t).wide_part + (uint64_t)(W.split - 1) * t * rows * 4;
+                    const size_t bytes = gemm_ws_layout(rows, cols, t).wide(W.split, t, rows, layer);
                     if (bytes > need) need = bytes;
                     has_wide = true;
                 }
                 if (has_decoded) continue;
                 const GemmDecodedPlan D = gemm_decoded_choice(rows, cols, tiles, list, W);
                 if (D.slab_tiles == 0) continue;
-                const size_t bytes = gemm_ws_layout(rows, cols, t).decoded(D.split, t, rows) + D.slab_bytes;
+                const size_t bytes = gemm_ws_layout(rows, cols, t).decoded(D.split, t, rows, layer) + D.slab_bytes;
                 if (bytes > need) need = bytes;
                 has_decoded = true;
             }
@@ -289,7 +295,7 @@ struct GemmPlan {
     GemmChains chains;
     bool x_in_place;
 };
-inline GemmPlan gemm_plan(uint64_t rows, uint64_t cols, uint64_t n_tokens, bool list, size_t ws_bytes) {
+inline GemmPlan gemm_plan(uint64_t rows, uint64_t cols, uint64_t n_tokens, bool list, size_t ws_bytes, bool layer = false) {
     const uint64_t tok_tiles = (n_tokens + GEMM_TOKENS - 1) / GEMM_TOKENS;
     GemmPlan P;
     P.ws = gemm_ws_layout(rows, cols, n_tokens);
@@ -298,9 +304,9 @@ inline GemmPlan gemm_plan(uint64_t rows, uint64_t cols, uint64_t n_tokens, bool 
     P.chains = gemm_chains(rows, cols, n_tokens, list);
     P.x_in_place = P.wide.split == 0 && gemm_x_in_place(rows, cols, n_tokens, list);
     P.way = GEMM_NARROW;
-    if (P.decoded.slab_tiles > 0 && ws_bytes >= P.ws.decoded(P.decoded.split, n_tokens, rows) + P.decoded.slab_bytes)
+    if (P.decoded.slab_tiles > 0 && ws_bytes >= P.ws.decoded(P.decoded.split, n_tokens, rows, layer) + P.decoded.slab_bytes)
         P.way = GEMM_DECODED;
-    else if (P.wide.split > 0 && ws_bytes >= P.ws.wide_part + (uint64_t)(P.wide.split - 1) * n_tokens * rows * 4)
+    else if (P.wide.split > 0 && ws_bytes >= P.ws.wide(P.wide.split, n_tokens, rows, layer))
         P.way = GEMM_WIDE;
     return P;
 }

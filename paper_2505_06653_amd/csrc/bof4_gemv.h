@@ -19,6 +19,7 @@
 #include <cstdint>
 
 #include "bof4_device.h"
+#include "bof4_epilogue.h"
 
 namespace bof4 {
 
@@ -30,7 +31,7 @@ constexpr uint32_t GEMV_MAX_WAVES = 8;    // waves per workgroup: two per SIMD, 
 
 // strip_ptr[r * n_strips + s] = number of list entries with index < r * cols + s * GEMV_STRIP (the list is
 // ascending), for every row and strip, and one closing entry: rows * n_strips + 1 values.
-__global__ __launch_bounds__(256) void outlier_strip_offsets_kernel(const int64_t* __restrict__ out_idx,
+static __global__ __launch_bounds__(256) void outlier_strip_offsets_kernel(const int64_t* __restrict__ out_idx,
                                                                     uint32_t n_out, uint64_t rows, uint64_t cols,
                                                                     uint32_t n_strips,
                                                                     uint32_t* __restrict__ strip_ptr) {
@@ -48,7 +49,7 @@ __global__ __launch_bounds__(256) void outlier_strip_offsets_kernel(const int64_
 
 // The list in the form the product wants it: per entry its column and (value - m * level[code]), what the entry adds
 // to its row's sum per unit of x.  An entry outside the matrix adds nothing.
-__global__ __launch_bounds__(256) void outlier_delta_kernel(const uint8_t* __restrict__ codes8,
+static __global__ __launch_bounds__(256) void outlier_delta_kernel(const uint8_t* __restrict__ codes8,
                                                             const uint16_t* __restrict__ scales, uint64_t n,
                                                             uint64_t cols, uint32_t log2_block, CodebookArgs cb,
                                                             const int64_t* __restrict__ out_idx,
@@ -78,13 +79,13 @@ __device__ __forceinline__ uint32_t byte_of(uint32_t v) {
 
 // One workgroup: rows [blockIdx.x * rc, ...) of the matrix; wave w takes strips w, w + waves, ... one after the other.
 // U rows are in flight per wave.
-template <int T, bool OUTLIERS>
+template <int T, bool OUTLIERS, class Out>
 __global__ __launch_bounds__(64 * GEMV_MAX_WAVES, T <= 2 ? 4 : T == 3 ? 3 : 2) void gemv_kernel(const uint4* __restrict__ codes, const uint16_t* __restrict__ scales,
                                                     uint32_t rows, uint32_t cols, uint32_t log2_block, uint32_t rc,
                                                     uint32_t n_strips, CodebookArgs cb,
                                                     const uint32_t* __restrict__ strip_ptr,
                                                     const uint2* __restrict__ entries, uint32_t n_out,
-                                                    const uint16_t* __restrict__ x, float* __restrict__ y) {
+                                                    const uint16_t* __restrict__ x, Out out) {
     constexpr uint32_t U = T >= 2 ? 1 : (OUTLIERS ? 2 : 4);  // measured best for each variant
     struct Shared {  // one object, so that the table sits at LDS offset 0 (reachable by an immediate offset)
         float tab[16];
@@ -244,7 +245,8 @@ __global__ __launch_bounds__(64 * GEMV_MAX_WAVES, T <= 2 ? 4 : T == 3 ? 3 : 2) v
         for (int t = 0; t < T; ++t) {
             float s = 0.0f;
             for (uint32_t p = 0; p < n_waves; ++p) s += sh.part[(p * rc + lane) * T + t];  // waves in order
-            y[(uint64_t)t * rows + r0 + lane] = s;
+            if constexpr (Out::LAYER) out.template store<1>(t, r0 + lane, rows, &s);
+            else out.first[(uint64_t)t * rows + r0 + lane] = s;
         }
     }
 }

@@ -1,0 +1,181 @@
+// bof4_linear.h - the gradients of a linear layer with a quantised matrix (bof4_epilogue.h has the layer's forward side):
+//
+//   dz = dy * mul * act'(z),   dx = dz W^,   dmul = dy * act(z),   dbias = sum over the tokens of dz.
+//
+// dx contracts over the rows of W^, so the matrix cores want it turned.  A call works in two steps, as the product for many
+// tokens does whose matrix is decoded first: linear_turn_kernel decodes the packed matrix into the operands of W^^T, in
+// slabs that stay in the cache behind the L2s, and gemm_decoded_kernel multiplies them with dz.  dz is rounded to bfloat16
+// once, which is what the matrix cores take: each term is off by 2^-9 of itself at most, as far as dx's own rounding to
+// bfloat16 (without activation and factor dz is dy, and nothing is rounded).  linear_dz_kernel makes it from dy in the
+// order of the operands, and dmul and dbias on the way.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "bof4_epilogue.h"
+#include "bof4_gemm.h"
+
+namespace bof4 {
+
+struct LinearGradArgs {
+    const void *dy, *pre, *mul;  // pre, mul null: not there (pre is there where act or dmul asks for it)
+    void* dmul;                  // null: not wanted
+    float* dbias_parts;          // null: not wanted
+    uint64_t ld_dy, ld_pre, ld_mul, ld_dmul;
+    uint32_t act;
+    bool dy_bf16, pre_bf16, mul_bf16, dmul_bf16;
+    bool wide;  // four neighbouring elements of every tensor are aligned to their size
+};
+
+// dz in the products' order (gemm_pack_x_kernel's, rows in the place of columns): a workgroup takes a chunk of 64 rows and
+// `tiles_per_range` tiles of 32 tokens, eight threads per token, which read 128 consecutive bytes and write 16-byte words of
+// which eight neighbouring tokens make up 128.  Bound by memory: 2000 tokens x 11008 rows with factor, activation and dmul.
+constexpr uint32_t LINEAR_MOST_RANGES = 64;  // parts of dbias at most
+__global__ __launch_bounds__(256) void linear_dz_kernel(LinearGradArgs a, uint32_t n_tokens, uint32_t rows, uint32_t n_chunks,
+                                                        uint32_t tok_tiles, uint32_t tiles_per_range, uint4* __restrict__ xp) {
+    __shared__ float sums[32][65];
+    const uint32_t tid = threadIdx.x, word = tid & 7, token_in_tile = tid >> 3, chunk = blockIdx.x;
+    const uint32_t row = chunk * GEMM_CHUNK + 8 * word;
+    float bias[8] = {};
+    const uint32_t tile1 = min(tok_tiles, (blockIdx.y + 1) * tiles_per_range);
+    for (uint32_t tile = blockIdx.y * tiles_per_range; tile < tile1; ++tile) {
+        const uint64_t t = tile * GEMM_TOKENS + token_in_tile;
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+        if (t < n_tokens) {
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) {
+                const uint32_t r = row + 4 * h;
+                if (r >= rows) break;
+                const uint32_t n = rows - r;
+                const bool whole = a.wide && n >= 4;
+                float dy[4], z[4] = {}, f[4], value[4], slope[4];
+                load_row<4>(a.dy, t * a.ld_dy + r, a.dy_bf16, whole, n, dy);
+                if (a.pre) load_row<4>(a.pre, t * a.ld_pre + r, a.pre_bf16, whole, n, z);
+                if (a.mul) load_row<4>(a.mul, t * a.ld_mul + r, a.mul_bf16, whole, n, f);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    activation_slope(a.act, z[i], value[i], slope[i]);
+                    value[i] *= dy[i];
+                    if (a.mul) dy[i] *= f[i];
+                    if (a.act != ACT_NONE) dy[i] *= slope[i];
+                    if ((uint32_t)i >= n) dy[i] = 0.0f;
+                    bias[4 * h + i] += dy[i];
+                }
+                if (a.dmul) store_row<4>(a.dmul, t * a.ld_dmul + r, a.dmul_bf16, whole, n, value);
+                w[2 * h] = gemm_pack_bf16(dy[0], dy[1]);
+                w[2 * h + 1] = gemm_pack_bf16(dy[2], dy[3]);
+            }
+        }
+        xp[((uint64_t)tile * n_chunks + chunk) * GEMM_TILE_WORDS + (word & 3) * 64 + (word >> 2) * 32 + token_in_tile] =
+            make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    if (!a.dbias_parts) return;
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) sums[token_in_tile][8 * word + i] = bias[i];
+    __syncthreads();
+    if (tid < GEMM_CHUNK && chunk * GEMM_CHUNK + tid < rows) {
+        float s = 0.0f;
+        for (uint32_t k = 0; k < 32; ++k) s += sums[k][tid];
+        a.dbias_parts[(uint64_t)blockIdx.y * rows + chunk * GEMM_CHUNK + tid] = s;
+    }
+}
+__global__ __launch_bounds__(256) void linear_dbias_kernel(const float* __restrict__ parts, uint32_t n_parts, uint32_t rows,
+                                                           float* __restrict__ dbias) {
+    const uint32_t row = blockIdx.x * 256 + threadIdx.x;
+    if (row >= rows) return;
+    double s = 0.0;
+    for (uint32_t k = 0; k < n_parts; ++k) s += parts[(uint64_t)k * rows + row];
+    dbias[row] = (float)s;
+}
+
+// W^^T in the order of the operands: 4096-byte tiles of 32 columns x 64 rows, from the packed tiles of 32 rows x 64 columns.
+// A wave turns 64 rows x 64 columns: it decodes as gemm_decode_kernel does (lane = row, 32 columns), puts neighbouring rows
+// of a column together with its neighbour lane (one lane exchange and one byte permutation per two weights), parks the
+// pairs in LDS by column, writes the tiles' list entries over their placeholders there and reads eight rows of a column at
+// a time.  A column takes LINEAR_TURN_LD bytes, so that sixteen lanes' 16-byte reads fall into different banks.
+constexpr uint32_t LINEAR_TURN_WAVES = 4, LINEAR_TURN_LD = 144;
+template <bool OUTLIERS>
+__global__ __launch_bounds__(64 * LINEAR_TURN_WAVES) void linear_turn_kernel(
+    const char* __restrict__ packed, uint32_t first_ct, uint32_t n_ct, uint32_t n_chunks, uint32_t row_chunks, CodebookArgs cb,
+    const uint32_t* __restrict__ list_ptr, const uint32_t* __restrict__ entries, uint32_t n_out, GemmListGeometry lg,
+    uint32_t row_tiles, uint4* __restrict__ decoded) {
+    struct Shared {
+        float tab[16];
+        uint4 turned[LINEAR_TURN_WAVES][64 * LINEAR_TURN_LD / 16];
+    };
+    __shared__ __attribute__((aligned(16))) Shared sh;
+    const uint32_t tid = threadIdx.x, lane = tid & 63;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (tid < 16) sh.tab[tid] = cb.lv32[tid];
+    __syncthreads();
+    const char* tab = reinterpret_cast<const char*>(sh.tab);
+    const uint64_t job = (uint64_t)blockIdx.x * LINEAR_TURN_WAVES + wave;
+    if (job >= (uint64_t)((n_ct + 1) / 2) * row_chunks) return;
+    const uint32_t ct_local = 2 * (uint32_t)(job / row_chunks), rc = (uint32_t)(job % row_chunks);
+    const uint32_t ch = (first_ct + ct_local) / 2;  // (first_ct is even)
+    uint4 q[2];
+    uint16_t m[2];
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) {
+        const char* tile = packed + ((uint64_t)(2 * rc + k) * n_chunks + ch) * GEMM_TILE_BYTES;
+        q[k] = load_stream(reinterpret_cast<const uint4*>(tile) + lane);
+        m[k] = __builtin_nontemporal_load(reinterpret_cast<const uint16_t*>(tile + 1024) + lane);
+    }
+    uint32_t lo[2] = {}, n_en[2] = {};
+    if (OUTLIERS) {
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {
+            if (2 * rc + k >= row_tiles) continue;  // wave-uniform
+            uint32_t hi;
+            gemm_list_range(list_ptr + (uint64_t)(2 * rc + k) * lg.n_groups + (ch >> lg.log2_group), n_out, lg.log2_group, lo[k], hi);
+            n_en[k] = hi - lo[k];
+        }
+    }
+    char* turned = reinterpret_cast<char*>(sh.turned[wave]);
+    const uint32_t odd = lane & 1u, pick = odd ? 0x03020706u : 0x05040100u;
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) {
+        const float msc = f16_bits_to_f32(m[k]);
+        const uint32_t w[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+        // the lane's pair of rows; even lanes keep the even columns, odd lanes the odd ones
+        char* at = turned + (32 * (lane >> 5) + odd) * LINEAR_TURN_LD + (16 * k + ((lane & 31u) >> 1)) * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t even = (w[j] << 2) & 0x3c3c3c3cu, odds = (w[j] >> 2) & 0x3c3c3c3cu;
+            const uint32_t oe[4] = {byte_of<0>(even), byte_of<1>(even), byte_of<2>(even), byte_of<3>(even)};
+            const uint32_t oo[4] = {byte_of<0>(odds), byte_of<1>(odds), byte_of<2>(odds), byte_of<3>(odds)};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float le = *reinterpret_cast<const float*>(tab + oe[i]);
+                const float lv = *reinterpret_cast<const float*>(tab + oo[i]);
+                const uint32_t mine = gemm_pack_bf16(msc * le, msc * lv);  // the decoder's product and rounding
+                const uint32_t other = (uint32_t)__builtin_amdgcn_mov_dpp((int)mine, 0xb1, 0xf, 0xf, true);  // lane ^ 1
+                *reinterpret_cast<uint32_t*>(at + (8 * j + 2 * i) * LINEAR_TURN_LD) = __builtin_amdgcn_perm(other, mine, pick);
+            }
+        }
+    }
+    wave_lds_fence();
+    if (OUTLIERS) {
+        const uint32_t place = ch & ((1u << lg.log2_group) - 1u);
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k)
+            for (uint32_t i = lane; i < n_en[k]; i += 64u) {
+                const uint32_t e = entries[lo[k] + i], at = (e >> 16) & 2047u;
+                if ((e >> 27) != place) continue;
+                const uint32_t col = 32 * ((at >> 8) & 1u) + 8 * (at >> 9) + (at & 7u), row = 32 * k + ((at >> 3) & 31u);
+                *reinterpret_cast<uint16_t*>(turned + col * LINEAR_TURN_LD + 2 * row) = (uint16_t)e;
+            }
+        wave_lds_fence();
+    }
+#pragma unroll
+    for (uint32_t t = 0; t < 2; ++t) {
+        if (ct_local + t >= n_ct) break;  // wave-uniform
+        uint4* out = decoded + ((uint64_t)(ct_local + t) * row_chunks + rc) * GEMM_TILE_WORDS + lane;
+        const char* from = turned + (32 * t + (lane & 31u)) * LINEAR_TURN_LD + 64 * (lane >> 5);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out[64 * j] = *reinterpret_cast<const uint4*>(from + 16 * j);
+    }
+}
+
+}  // namespace bof4

@@ -4,7 +4,7 @@ import ctypes
 
 import pytest
 
-from paper_2505_06653_amd import binding
+from paper_2505_06653_amd import binding, codebooks
 
 F32, BF16 = 0, 1
 
@@ -57,3 +57,92 @@ def backward(logits=P, kind=F32, n=4, vocab=100, ld=100, stats=P, target=P, d_lp
 def test_token_logprobs_backward_refuses(bad):
     assert backward(**bad) == binding.BOF4_ERR_ARG
     assert b"bof4_token_logprobs_backward" in binding.lib().bof4_last_error()
+
+
+# ------------------------------------------------------------------------------------------------ linear layers
+CB = codebooks.array(codebooks.BOF4S_MSE[64])
+CBP = CB.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
+BAD_CB = CB[::-1].copy()
+BAD_CBP = BAD_CB.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
+
+
+def record(kind, **fields):
+    r = kind()
+    for k, v in fields.items():
+        setattr(r, k, v.value if isinstance(v, ctypes.c_void_p) else v)
+    return r
+
+
+def layer(**kw):
+    return record(binding.Layer, **{**dict(y_dev=0x40000, y_type=BF16, ld_y=64), **kw})
+
+
+def gemv_linear(codes=P, scales=P, rows=64, cols=128, block=64, cb=CBP, table=None, k=0, x=at(0x20000), n=2, lay=None, null=False, **kw):
+    return binding.lib().bof4_gemv_linear(codes, scales, rows, cols, block, cb, table, k, x, n,
+                                          None if null else lay or layer(**kw), None)
+
+
+def gemm_linear(packed=P, rows=64, cols=128, cb=CBP, table=None, k=0, x=at(0x20000), n=2, ws=at(0x80000), size=1 << 40, null=False, **kw):
+    return binding.lib().bof4_gemm_linear(packed, rows, cols, cb, table, k, x, n, None if null else layer(**kw), ws, size, None)
+
+
+BAD_LAYERS = [dict(null=True), dict(y_dev=None), dict(act=5), dict(y_type=2), dict(y_dev=0x40001), dict(ld_y=63),
+              dict(bias_dev=0x50001, bias_type=BF16), dict(bias_dev=0x50002, bias_type=F32), dict(bias_dev=0x50000, bias_type=3),
+              dict(mul_dev=0x50000, mul_type=BF16, ld_mul=63), dict(mul_dev=0x50000, mul_type=9, ld_mul=64),
+              dict(residual_dev=0x50000, ld_residual=10), dict(residual_dev=0x50002, residual_type=F32, ld_residual=64),
+              dict(pre_dev=0x50002, pre_type=F32, ld_pre=64), dict(pre_dev=0x40000, pre_type=BF16, ld_pre=64),
+              dict(residual_dev=0x40000, residual_type=F32, ld_residual=64), dict(residual_dev=0x40000, residual_type=BF16, ld_residual=65),
+              dict(mul_dev=0x40000, mul_type=F32, ld_mul=64), dict(bias_dev=0x40000, bias_type=BF16), dict(y_dev=0x20000)]
+
+
+@pytest.mark.parametrize("bad", BAD_LAYERS + [
+    dict(codes=None), dict(scales=None), dict(x=None), dict(rows=0), dict(cols=0), dict(cols=96), dict(block=48), dict(n=0),
+    dict(rows=(1 << 30) + 1, ld_y=1 << 31), dict(cols=32832), dict(cb=BAD_CBP), dict(k=3), dict(k=1 << 32, table=P), dict(codes=at(0x10008)),
+    dict(x=at(0x20002)), dict(scales=at(0x10001)), dict(table=at(0x10004), k=1)])
+def test_gemv_linear_refuses(bad):
+    assert gemv_linear(**bad) == binding.BOF4_ERR_ARG
+    assert b"linear" in binding.lib().bof4_last_error()
+
+
+@pytest.mark.parametrize("bad", BAD_LAYERS + [
+    dict(packed=None), dict(x=None), dict(ws=None), dict(rows=0), dict(cols=0), dict(cols=100), dict(n=0), dict(n=65537),
+    dict(rows=(1 << 30) + 1, ld_y=1 << 31), dict(cols=32800), dict(cb=BAD_CBP), dict(k=3), dict(k=1 << 32, table=P), dict(packed=at(0x10008)),
+    dict(x=at(0x20002)), dict(ws=at(0x80010)), dict(table=at(0x10004), k=1)])
+def test_gemm_linear_refuses(bad):
+    assert gemm_linear(**bad) == binding.BOF4_ERR_ARG
+    assert b"linear" in binding.lib().bof4_last_error()
+
+
+def gemm_linear_backward(packed=P, rows=64, cols=128, cb=CBP, table=None, k=0, n=2, ws=at(0x80000), size=1 << 40, null=False, **kw):
+    g = record(binding.LayerGradient, **{**dict(dy_dev=0x20000, dy_type=BF16, ld_dy=64, dx_dev=0x40000, dx_type=BF16, ld_dx=128), **kw})
+    return binding.lib().bof4_gemm_linear_backward(packed, rows, cols, cb, table, k, n, None if null else g, ws, size, None)
+
+
+MUL, PRE = dict(mul_dev=0x50000, mul_type=BF16, ld_mul=64), dict(pre_dev=0x60000, pre_type=BF16, ld_pre=64)
+DMUL = dict(dmul_dev=0x70000, dmul_type=BF16, ld_dmul=64)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(null=True), dict(packed=None), dict(ws=None), dict(dy_dev=None), dict(dx_dev=None), dict(rows=0), dict(cols=0), dict(cols=100),
+    dict(n=0), dict(n=65537), dict(rows=(1 << 18) + 1, ld_dy=1 << 20), dict(cols=32800, ld_dx=1 << 16), dict(cb=BAD_CBP), dict(k=3),
+    dict(k=1 << 32, table=P), dict(packed=at(0x10008)), dict(ws=at(0x80010)), dict(table=at(0x10004), k=1), dict(act=5), dict(act=1),
+    dict(ld_dy=63), dict(ld_dx=127), dict(dy_type=2), dict(dx_type=2), dict(dy_dev=0x20001), dict(dx_dev=0x40001), {**DMUL}, {**DMUL, **MUL},
+    {**DMUL, **PRE}, {**MUL, "ld_mul": 63}, {**PRE, "ld_pre": 63}, {**MUL, **PRE, **DMUL, "ld_dmul": 63}, {**MUL, **PRE, **DMUL, "dmul_dev": 0x40000},
+    {**MUL, **PRE, **DMUL, "dmul_dev": 0x20000, "dmul_type": F32}, {**MUL, **PRE, **DMUL, "dmul_dev": 0x50000, "ld_dmul": 65},
+    dict(dbias_dev=0x30002), dict(dbias_dev=0x40000)])
+def test_gemm_linear_backward_refuses(bad):
+    assert gemm_linear_backward(**bad) == binding.BOF4_ERR_ARG
+    assert b"bof4_gemm_linear_backward" in binding.lib().bof4_last_error()
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 32), (1001, 1504), (300, 28672), (28672, 300 // 32 * 32), (11008, 4096), (128256, 4096), (1 << 18, 32)])
+def test_linear_workspaces_never_fall_as_tokens_rise_and_hold_the_product(rows, cols):
+    L = binding.lib()
+    for f in (L.bof4_gemm_linear_workspace_bytes, L.bof4_gemm_linear_backward_workspace_bytes):
+        sizes = [f(rows, cols, n) for n in (1, 5, 31, 32, 33, 100, 128, 129, 257, 500, 1000, 2000, 3000, 9000, 65536)]
+        assert sizes == sorted(sizes) and sizes[0] > 0
+    assert L.bof4_gemm_linear_workspace_bytes(rows, cols, 500) >= L.bof4_gemm_workspace_bytes(rows, cols, 500)
+    assert gemm_linear(rows=rows, cols=cols, n=500, ld_y=rows, size=1000) == binding.BOF4_ERR_WORKSPACE
+    assert gemm_linear_backward(rows=rows, cols=cols, n=500, ld_dy=rows, ld_dx=cols, size=1000) == binding.BOF4_ERR_WORKSPACE
+    assert L.bof4_gemm_linear_workspace_bytes(0, cols, 5) == 0 and L.bof4_gemm_linear_backward_workspace_bytes(rows, cols, 0) == 0
+    assert L.bof4_gemm_linear_backward_workspace_bytes((1 << 18) + 1, cols, 5) == 0
