@@ -5,6 +5,7 @@ the C entry points.  A missing library is an error (there is no fallback of any 
 """
 import ctypes
 import os
+import struct
 
 import numpy as np
 import torch
@@ -62,18 +63,9 @@ class MaeStats(ctypes.Structure):
                 "n_used": int(self.n_used), "n_outliers": int(self.n_outliers)}
 
 
-class Layer(ctypes.Structure):
-    """bof4_layer of include/bof4.h."""
-    _fields_ = ([("act", ctypes.c_uint32)] + [(k + "_type", ctypes.c_uint32) for k in ("bias", "mul", "residual", "y", "pre")]
-                + [(k + "_dev", ctypes.c_void_p) for k in ("bias", "mul", "residual", "y", "pre")]
-                + [("ld_" + k, ctypes.c_uint64) for k in ("mul", "residual", "y", "pre")])
-
-
-class LayerGradient(ctypes.Structure):
-    """bof4_layer_gradient of include/bof4.h."""
-    _fields_ = ([("act", ctypes.c_uint32)] + [(k + "_type", ctypes.c_uint32) for k in ("dy", "pre", "mul", "dmul", "dx")]
-                + [(k + "_dev", ctypes.c_void_p) for k in ("dy", "pre", "mul", "dmul", "dbias", "dx")]
-                + [("ld_" + k, ctypes.c_uint64) for k in ("dy", "pre", "mul", "dmul", "dx")])
+# bof4_layer and bof4_layer_gradient of include/bof4.h, packed: act and five types, five or six addresses, row strides
+LAYER = struct.Struct("@6I5P4Q")
+LAYER_GRADIENT = struct.Struct("@6I6P5Q")
 
 
 _lib = None
@@ -153,11 +145,11 @@ def lib():
         L.bof4_gemm_workspace_bytes.argtypes = [ctypes.c_uint64, ctypes.c_uint64, ctypes.c_uint32]
         u32, u64, size = ctypes.c_uint32, ctypes.c_uint64, ctypes.c_size_t
         L.bof4_gemv_linear.restype = ctypes.c_int
-        L.bof4_gemv_linear.argtypes = [vp, vp, u64, u64, u32, f64p, vp, u64, vp, u32, ctypes.POINTER(Layer), vp]
+        L.bof4_gemv_linear.argtypes = [vp, vp, u64, u64, u32, f64p, vp, u64, vp, u32, vp, vp]
         L.bof4_gemm_linear.restype = ctypes.c_int
-        L.bof4_gemm_linear.argtypes = [vp, u64, u64, f64p, vp, u64, vp, u32, ctypes.POINTER(Layer), vp, size, vp]
+        L.bof4_gemm_linear.argtypes = [vp, u64, u64, f64p, vp, u64, vp, u32, vp, vp, size, vp]
         L.bof4_gemm_linear_backward.restype = ctypes.c_int
-        L.bof4_gemm_linear_backward.argtypes = [vp, u64, u64, f64p, vp, u64, u32, ctypes.POINTER(LayerGradient), vp, size, vp]
+        L.bof4_gemm_linear_backward.argtypes = [vp, u64, u64, f64p, vp, u64, u32, vp, vp, size, vp]
         for name in ("bof4_gemm_linear_workspace_bytes", "bof4_gemm_linear_backward_workspace_bytes"):
             getattr(L, name).restype = size
             getattr(L, name).argtypes = [u64, u64, u32]
@@ -643,29 +635,26 @@ def bof4_dequantize(codes, scales, n, block, cb, out_idx=None, out_val=None, out
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}  # BOF4_F32, BOF4_BF16
 
 
-def _tensor(t, name, dtypes, shape=None):
-    """A device tensor of one of `dtypes` and of that shape, its last dimension contiguous, on the current device (the
-    library enqueues on that).  Returns its address."""
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} must be on the current GPU, not on {t.device}")
-    if not t.is_contiguous() and t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name} must be contiguous in its last dimension")
+def _tensor(t, name, dtypes, shape, dev):
+    """The address of a tensor of one of `dtypes` and of that shape (None: any), its last dimension contiguous, on the current
+    device `dev` (the library enqueues on that)."""
+    if t.get_device() != dev or t.dtype not in dtypes or (shape is not None and t.shape != shape) or \
+            (not t.is_contiguous() and t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must be of {' or '.join(str(d) for d in dtypes)}, of the shape {shape or tuple(t.shape)}, on the "
+                         f"current GPU and contiguous in its last dimension: got {t.dtype}, {tuple(t.shape)}, {t.device}, strides "
+                         f"{t.stride()}")
     return t.data_ptr()
 
 
 def _row_stride(t):
     """Elements from one row of a 2-d tensor to the next (a single row's stride says nothing)."""
-    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.shape[1]), 1)
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-def _flat(t, name, dtypes, shape=None):
+def _flat(t, name, dtypes, shape, dev):
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    return _tensor(t, name, dtypes, shape)
+    return _tensor(t, name, dtypes, shape, dev)
 
 
 _F32, _I64, _U8 = (torch.float32,), (torch.int64,), (torch.uint8,)
@@ -674,7 +663,7 @@ _F32, _I64, _U8 = (torch.float32,), (torch.int64,), (torch.uint8,)
 def _scratch(ws, nbytes, device, stream):
     """The caller's workspace, or one of `nbytes` that the allocator keeps until `stream` is done with it."""
     if ws is not None:
-        _flat(ws, "ws", _U8)
+        _flat(ws, "ws", _U8, None, torch.cuda.current_device())
         return ws
     ws = torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
     if stream is not None:
@@ -691,32 +680,28 @@ def _activation(act):
     return ACTIVATIONS[act]
 
 
-def _layer_input(x, cols):
+def _layer_input(x, cols, gpu):
     x2 = x if x.dim() == 2 else x[None, :]
-    if x2.dtype != torch.bfloat16 or x2.shape[1] != cols or not x2.is_contiguous():
-        raise ValueError("x must be a contiguous bfloat16 tensor of [n_tokens, cols]")
-    _tensor(x2, "x", _TYPES)
+    if x2.dtype != torch.bfloat16 or x2.shape[1] != cols or not x2.is_contiguous() or x2.get_device() != gpu:
+        raise ValueError("x must be a contiguous bfloat16 tensor of [n_tokens, cols] on the current GPU")
     return x2
 
 
-def _rows_of(record, key, t, shape):
-    """Address, type and row stride of a tensor of tokens x rows (or None) into the record's fields."""
-    if t is not None:
-        setattr(record, key + "_dev", _tensor(t, key, _TYPES, shape))
-        setattr(record, key + "_type", _TYPES[t.dtype])
-        setattr(record, "ld_" + key, _row_stride(t))
-
-
-def _layer(n_tokens, rows, bias, act, mul, residual, pre, out):
-    layer, shape = Layer(), (n_tokens, rows)
-    layer.act = _activation(act)
+def _layer(n_tokens, rows, bias, act, mul, residual, pre, out, gpu):
+    shape = (n_tokens, rows)
+    bias_at = mul_at = residual_at = pre_at = bias_type = mul_type = residual_type = pre_type = ld_mul = ld_residual = ld_pre = 0
     if bias is not None:
-        layer.bias_dev, layer.bias_type = _flat(bias, "bias", _TYPES, (rows,)), _TYPES[bias.dtype]
-    _rows_of(layer, "mul", mul, shape)
-    _rows_of(layer, "residual", residual, shape)
-    _rows_of(layer, "pre", pre, shape)
-    _rows_of(layer, "y", out, shape)
-    return layer
+        bias_at, bias_type = _flat(bias, "bias", _TYPES, (rows,), gpu), _TYPES[bias.dtype]
+    if mul is not None:
+        mul_at, mul_type, ld_mul = _tensor(mul, "mul", _TYPES, shape, gpu), _TYPES[mul.dtype], _row_stride(mul)
+    if residual is not None:
+        residual_at, residual_type = _tensor(residual, "residual", _TYPES, shape, gpu), _TYPES[residual.dtype]
+        ld_residual = _row_stride(residual)
+    if pre is not None:
+        pre_at, pre_type, ld_pre = _tensor(pre, "pre", _TYPES, shape, gpu), _TYPES[pre.dtype], _row_stride(pre)
+    out_at = _tensor(out, "out", _TYPES, shape, gpu)
+    return LAYER.pack(_activation(act), bias_type, mul_type, residual_type, _TYPES[out.dtype], pre_type, bias_at, mul_at,
+                      residual_at, out_at, pre_at, ld_mul, ld_residual, _row_stride(out), ld_pre)
 
 
 def bof4_gemv_linear(codes, scales, rows, cols, block, cb, x, table=None, n_outliers=0, bias=None, act="none", mul=None,
@@ -725,13 +710,14 @@ def bof4_gemv_linear(codes, scales, rows, cols, block, cb, x, table=None, n_outl
     residual, pre, out [n_tokens, rows] (rows of any stride): bfloat16 or float32 each.  act: a key of ACTIVATIONS.  `pre`: a
     tensor that receives x W~^T + bias; `out`: the result's, may be mul or the residual (else of `out_dtype`)."""
     cb, cbp = _cb(cb)
-    x2 = _layer_input(x, cols)
-    n_tokens, k = int(x2.shape[0]), int(n_outliers)
+    gpu = torch.cuda.current_device()
+    x2 = _layer_input(x, cols, gpu)
+    n_tokens, k = x2.shape[0], int(n_outliers)
     if k and table is None:
         raise ValueError("outliers need their table (bof4_gemv_outlier_table)")
     if out is None:
         out = torch.empty((n_tokens, rows), dtype=out_dtype, device=x.device)
-    layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out)
+    layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out, gpu)
     _check(lib().bof4_gemv_linear(codes.data_ptr(), scales.data_ptr(), rows, cols, block, cbp, table.data_ptr() if k else None, k,
                                   x2.data_ptr(), n_tokens, layer, _stream(stream)))
     return out
@@ -746,15 +732,16 @@ def bof4_gemm_linear(packed, rows, cols, cb, x, table=None, n_outliers=0, bias=N
     """y = act(x W^^T + bias) * mul + residual for many tokens; matrix, x, table as for bof4_gemm, the rest as for
     bof4_gemv_linear; `ws`: optional uint8 device tensor of bof4_gemm_linear_workspace_bytes(...) bytes."""
     cb, cbp = _cb(cb)
-    x2 = _layer_input(x, cols)
+    gpu = torch.cuda.current_device()
+    x2 = _layer_input(x, cols, gpu)
     if packed.numel() < bof4_gemm_packed_bytes(rows, cols):
         raise ValueError("packed matrix too small for rows x cols (bof4_gemm_pack)")
-    n_tokens, k = int(x2.shape[0]), int(n_outliers)
+    n_tokens, k = x2.shape[0], int(n_outliers)
     if k and table is None:
         raise ValueError("outliers need their table (bof4_gemm_outlier_table)")
     if out is None:
         out = torch.empty((n_tokens, rows), dtype=out_dtype, device=x.device)
-    layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out)
+    layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out, gpu)
     ws = _scratch(ws, 0 if ws is not None else bof4_gemm_linear_workspace_bytes(rows, cols, n_tokens), x.device, stream)
     _check(lib().bof4_gemm_linear(packed.data_ptr(), rows, cols, cbp, table.data_ptr() if k else None, k, x2.data_ptr(),
                                   n_tokens, layer, ws.data_ptr(), ws.numel(), _stream(stream)))
@@ -780,15 +767,19 @@ def bof4_gemm_linear_backward(packed, rows, cols, cb, dy, table=None, n_outliers
         raise ValueError("outliers need their table (bof4_gemm_outlier_table)")
     if out is None:
         out = torch.empty((n_tokens, cols), dtype=out_dtype, device=dy.device)
-    g, shape = LayerGradient(), (n_tokens, rows)
-    g.act = _activation(act)
-    _rows_of(g, "dy", dy, shape)
-    _rows_of(g, "pre", pre, shape)
-    _rows_of(g, "mul", mul, shape)
-    _rows_of(g, "dmul", dmul, shape)
-    _rows_of(g, "dx", out, (n_tokens, cols))
+    gpu, shape = torch.cuda.current_device(), (n_tokens, rows)
+    pre_at = mul_at = dmul_at = dbias_at = pre_type = mul_type = dmul_type = ld_pre = ld_mul = ld_dmul = 0
+    dy_at, dx_at = _tensor(dy, "dy", _TYPES, shape, gpu), _tensor(out, "out", _TYPES, (n_tokens, cols), gpu)
+    if pre is not None:
+        pre_at, pre_type, ld_pre = _tensor(pre, "pre", _TYPES, shape, gpu), _TYPES[pre.dtype], _row_stride(pre)
+    if mul is not None:
+        mul_at, mul_type, ld_mul = _tensor(mul, "mul", _TYPES, shape, gpu), _TYPES[mul.dtype], _row_stride(mul)
+    if dmul is not None:
+        dmul_at, dmul_type, ld_dmul = _tensor(dmul, "dmul", _TYPES, shape, gpu), _TYPES[dmul.dtype], _row_stride(dmul)
     if dbias is not None:
-        g.dbias_dev = _flat(dbias, "dbias", _F32, (rows,))
+        dbias_at = _flat(dbias, "dbias", _F32, (rows,), gpu)
+    g = LAYER_GRADIENT.pack(_activation(act), _TYPES[dy.dtype], pre_type, mul_type, dmul_type, _TYPES[out.dtype], dy_at, pre_at,
+                            mul_at, dmul_at, dbias_at, dx_at, _row_stride(dy), ld_pre, ld_mul, ld_dmul, _row_stride(out))
     ws = _scratch(ws, 0 if ws is not None else bof4_gemm_linear_backward_workspace_bytes(rows, cols, n_tokens), dy.device, stream)
     _check(lib().bof4_gemm_linear_backward(packed.data_ptr(), rows, cols, cbp, table.data_ptr() if k else None, k, n_tokens, g,
                                            ws.data_ptr(), ws.numel(), _stream(stream)))
@@ -803,7 +794,8 @@ def bof4_token_logprobs(logits, targets=None, top=0, ws=None, stream=None):
     """logits: float32 or bfloat16 [n_rows, vocab] on the device, rows of any stride; targets: int64 [n_rows] (below 0: no
     token asked for).  Returns (logprob float32 [n_rows] or None without targets, entropy float32 [n_rows], top_idx int64
     [n_rows, top] and top_logprob float32 [n_rows, top] or None with top = 0, stats float32 [n_rows, 2])."""
-    logits_at = _tensor(logits, "logits", _TYPES)
+    gpu = torch.cuda.current_device()
+    logits_at = _tensor(logits, "logits", _TYPES, None, gpu)
     if logits.dim() != 2:
         raise ValueError("logits must be [n_rows, vocab]")
     n, vocab = logits.shape
@@ -812,7 +804,7 @@ def bof4_token_logprobs(logits, targets=None, top=0, ws=None, stream=None):
         raise ValueError("top must not be negative")
     logprob = top_idx = top_logprob = targets_at = logprob_at = idx_at = top_at = None
     if targets is not None:
-        targets_at = _flat(targets, "targets", _I64, (n,))
+        targets_at = _flat(targets, "targets", _I64, (n,), gpu)
         logprob = torch.empty(n, dtype=f32, device=dev)
         logprob_at = logprob.data_ptr()
     entropy, stats = torch.empty(n, dtype=f32, device=dev), torch.empty((n, 2), dtype=f32, device=dev)
@@ -831,7 +823,8 @@ def bof4_token_logprobs_backward(logits, stats, targets=None, d_logprob=None, en
                                  out_dtype=None, stream=None):
     """The gradient by the logits, [n_rows, vocab], from bof4_token_logprobs' stats (and entropy) and the gradients of its
     logprob and entropy (float32 [n_rows]; None: that output is not used).  `out`: a tensor to fill, may be the logits."""
-    logits_at = _tensor(logits, "logits", _TYPES)
+    gpu = torch.cuda.current_device()
+    logits_at = _tensor(logits, "logits", _TYPES, None, gpu)
     if logits.dim() != 2:
         raise ValueError("logits must be [n_rows, vocab]")
     n, vocab = logits.shape
@@ -839,13 +832,13 @@ def bof4_token_logprobs_backward(logits, stats, targets=None, d_logprob=None, en
         raise ValueError("targets come with d_logprob, the entropy with d_entropy")
     targets_at = d_logprob_at = entropy_at = d_entropy_at = None
     if targets is not None:
-        targets_at, d_logprob_at = _flat(targets, "targets", _I64, (n,)), _flat(d_logprob, "d_logprob", _F32, (n,))
+        targets_at, d_logprob_at = _flat(targets, "targets", _I64, (n,), gpu), _flat(d_logprob, "d_logprob", _F32, (n,), gpu)
     if entropy is not None:
-        entropy_at, d_entropy_at = _flat(entropy, "entropy", _F32, (n,)), _flat(d_entropy, "d_entropy", _F32, (n,))
+        entropy_at, d_entropy_at = _flat(entropy, "entropy", _F32, (n,), gpu), _flat(d_entropy, "d_entropy", _F32, (n,), gpu)
     if out is None:
         out = torch.empty((n, vocab), dtype=out_dtype or logits.dtype, device=logits.device)
-    out_at = _tensor(out, "out", _TYPES, (n, vocab))
+    out_at = _tensor(out, "out", _TYPES, (n, vocab), gpu)
     _check(lib().bof4_token_logprobs_backward(logits_at, _TYPES[logits.dtype], n, vocab, _row_stride(logits),
-                                              _flat(stats, "stats", _F32, (n, 2)), targets_at, d_logprob_at, entropy_at,
+                                              _flat(stats, "stats", _F32, (n, 2), gpu), targets_at, d_logprob_at, entropy_at,
                                               d_entropy_at, out_at, _TYPES[out.dtype], _row_stride(out), _stream(stream)))
     return out

@@ -213,6 +213,17 @@ __device__ __forceinline__ void wave_lds_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// Two numbers rounded to bfloat16 (to nearest even), the first in the low half (one instruction).
+typedef __bf16 gemm_bf16x2 __attribute__((ext_vector_type(2)));
+typedef float gemm_f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t gemm_pack_bf16(float lo, float hi) {
+    gemm_f32x2 v = {lo, hi};
+    gemm_bf16x2 r = __builtin_convertvector(v, gemm_bf16x2);
+    uint32_t u;
+    __builtin_memcpy(&u, &r, 4);
+    return u;
+}
+
 // Slow, always-valid nearest-level search.
 __device__ __forceinline__ int assign_code_generic(float x, const CodebookArgs& cb) {
     int code = 0;

@@ -19,7 +19,10 @@ namespace bof4 {
 constexpr uint32_t ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_GELU_TANH = 3, ACT_SILU = 4, ACT_COUNT = 5;
 constexpr float GELU_TANH_A = 0.79788456080286536f, GELU_TANH_B = 0.044715f;  // sqrt(2 / pi)
 
-__device__ __forceinline__ float sigmoid(float q) { return __builtin_amdgcn_rcpf(1.0f + expf(-q)); }
+// exp with the error of the argument's product with log2 e, 1.5 |q| 2^-24 of itself: what that leaves in a sigmoid times its
+// argument is below 2^-24.
+__device__ __forceinline__ float short_exp(float q) { return __builtin_amdgcn_exp2f(q * 1.44269504088896341f); }
+__device__ __forceinline__ float sigmoid(float q) { return __builtin_amdgcn_rcpf(1.0f + short_exp(-q)); }
 // (1 + tanh t) / 2 is the sigmoid of 2 t: silu and the tanh form of gelu share it.
 __device__ __forceinline__ float activation(uint32_t act, float z) {
     if (act == ACT_NONE) return z;
@@ -38,7 +41,7 @@ __device__ __forceinline__ void activation_slope(uint32_t act, float z, float& v
     } else if (act == ACT_GELU) {
         const float cdf = 0.5f * (1.0f + erff(z * 0.70710678118654752f));
         value = z * cdf;
-        slope = fmaf(z, 0.39894228040143268f * expf(-0.5f * z * z), cdf);
+        slope = fmaf(z, 0.39894228040143268f * short_exp(-0.5f * z * z), cdf);
     } else {
         // (beyond 30 the tanh form's sigmoid is 0 or 1 in binary32; farther out its polynomial's slope would overflow)
         const bool silu = act == ACT_SILU;
@@ -51,7 +54,7 @@ __device__ __forceinline__ void activation_slope(uint32_t act, float z, float& v
 }
 
 // ------------------------------------------------------------------------------------------------ rows of either type
-// N neighbouring elements (1, 2 or 4) of a bfloat16 or binary32 row; `whole`: all of them there, aligned to their size.
+// N neighbouring elements (1, 2, 4 or 8) of a bfloat16 or binary32 row; `whole`: all of them there, aligned to their size.
 template <int N>
 __device__ __forceinline__ void load_row(const void* p, uint64_t i, bool bf16, bool whole, uint32_t n, float* v) {
     if (bf16) {
@@ -63,6 +66,13 @@ __device__ __forceinline__ void load_row(const void* p, uint64_t i, bool bf16, b
                 const uint2 t = *reinterpret_cast<const uint2*>(q);
                 w[0] = t.x;
                 w[1] = t.y;
+            }
+            if constexpr (N == 8) {
+                const uint4 t = *reinterpret_cast<const uint4*>(q);
+                w[0] = t.x;
+                w[1] = t.y;
+                w[2] = t.z;
+                w[3] = t.w;
             }
 #pragma unroll
             for (int k = 0; k < N; ++k) v[k] = k % 2 ? __uint_as_float(w[k / 2] & 0xffff0000u) : __uint_as_float(w[k / 2] << 16);
@@ -78,12 +88,15 @@ __device__ __forceinline__ void load_row(const void* p, uint64_t i, bool bf16, b
                 v[0] = t.x;
                 v[1] = t.y;
             }
-            if constexpr (N == 4) {
-                const float4 t = *reinterpret_cast<const float4*>(q);
-                v[0] = t.x;
-                v[1] = t.y;
-                v[2] = t.z;
-                v[3] = t.w;
+            if constexpr (N >= 4) {
+#pragma unroll
+                for (int k = 0; k < N; k += 4) {
+                    const float4 t = *reinterpret_cast<const float4*>(q + k);
+                    v[k] = t.x;
+                    v[k + 1] = t.y;
+                    v[k + 2] = t.z;
+                    v[k + 3] = t.w;
+                }
             }
         } else {
 #pragma unroll
@@ -96,10 +109,12 @@ __device__ __forceinline__ void store_row(void* p, uint64_t i, bool bf16, bool w
     if (bf16) {
         uint16_t* q = reinterpret_cast<uint16_t*>(p) + i;
         if (N > 1 && whole) {
-            if constexpr (N == 2) *reinterpret_cast<uint32_t*>(q) = f32_to_bf16_rne(v[0]) | (f32_to_bf16_rne(v[1]) << 16);
+            if constexpr (N == 2) *reinterpret_cast<uint32_t*>(q) = gemm_pack_bf16(v[0], v[1]);
             if constexpr (N == 4)
-                *reinterpret_cast<uint2*>(q) = make_uint2(f32_to_bf16_rne(v[0]) | (f32_to_bf16_rne(v[1]) << 16),
-                                                          f32_to_bf16_rne(v[2]) | (f32_to_bf16_rne(v[3]) << 16));
+                *reinterpret_cast<uint2*>(q) = make_uint2(gemm_pack_bf16(v[0], v[1]), gemm_pack_bf16(v[2], v[3]));
+            if constexpr (N == 8)
+                *reinterpret_cast<uint4*>(q) = make_uint4(gemm_pack_bf16(v[0], v[1]), gemm_pack_bf16(v[2], v[3]),
+                                                          gemm_pack_bf16(v[4], v[5]), gemm_pack_bf16(v[6], v[7]));
         } else {
 #pragma unroll
             for (int k = 0; k < N; ++k)
@@ -109,7 +124,10 @@ __device__ __forceinline__ void store_row(void* p, uint64_t i, bool bf16, bool w
         float* q = reinterpret_cast<float*>(p) + i;
         if (N > 1 && whole) {
             if constexpr (N == 2) *reinterpret_cast<float2*>(q) = make_float2(v[0], v[1]);
-            if constexpr (N == 4) *reinterpret_cast<float4*>(q) = make_float4(v[0], v[1], v[2], v[3]);
+            if constexpr (N >= 4) {
+#pragma unroll
+                for (int k = 0; k < N; k += 4) *reinterpret_cast<float4*>(q + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+            }
         } else {
 #pragma unroll
             for (int k = 0; k < N; ++k)
@@ -122,6 +140,8 @@ __device__ __forceinline__ void store_row(void* p, uint64_t i, bool bf16, bool w
 // As they are: the first part of a row's columns to `first`, the others behind each other to `more`.
 struct PlainOut {
     static constexpr bool LAYER = false;
+    template <int T>
+    struct Ahead {};
     float *first, *more;
     __device__ __forceinline__ float* part(uint32_t p, uint64_t n_tokens, uint32_t rows) const {
         return p == 0 ? first : more + (uint64_t)(p - 1) * n_tokens * rows;
@@ -141,6 +161,31 @@ struct LayerOut {
     float* parts;
     __device__ __forceinline__ float* part(uint32_t p, uint64_t n_tokens, uint32_t rows) const {
         return parts + (uint64_t)p * n_tokens * rows;
+    }
+    // What one row's results of T tokens take besides the sums, asked for ahead of them.
+    template <int T>
+    struct Ahead {
+        float bias, f[T], r[T];
+    };
+    template <int T>
+    __device__ __forceinline__ Ahead<T> ask(uint32_t row) const {
+        Ahead<T> a = {};
+        if (bias) load_row<1>(bias, row, bias_bf16, true, 1, &a.bias);
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            if (mul) load_row<1>(mul, (uint64_t)(token0 + t) * ld_mul + row, mul_bf16, true, 1, &a.f[t]);
+            if (residual) load_row<1>(residual, (uint64_t)(token0 + t) * ld_residual + row, residual_bf16, true, 1, &a.r[t]);
+        }
+        return a;
+    }
+    template <int T>
+    __device__ __forceinline__ void store_one(uint32_t t, uint32_t row, const Ahead<T>& a, float z) const {
+        if (bias) z += a.bias;
+        if (pre) store_row<1>(pre, (uint64_t)(token0 + t) * ld_pre + row, pre_bf16, true, 1, &z);
+        float v = activation(act, z);
+        if (mul) v *= a.f[t];
+        if (residual) v += a.r[t];
+        store_row<1>(y, (uint64_t)(token0 + t) * ld_y + row, y_bf16, true, 1, &v);
     }
     // The sums of N neighbouring rows (a multiple of N first) of one token: read first, then written, so that y may be
     // the residual or the factor itself.

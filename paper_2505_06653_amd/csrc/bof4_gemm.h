@@ -32,18 +32,8 @@
 namespace bof4 {
 
 typedef __bf16 gemm_bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 gemm_bf16x2 __attribute__((ext_vector_type(2)));
-typedef float gemm_f32x2 __attribute__((ext_vector_type(2)));
 typedef float gemm_f32x2_any __attribute__((ext_vector_type(2), aligned(4)));  // two floats anywhere
 typedef float gemm_f32x16 __attribute__((ext_vector_type(16)));
-
-__device__ __forceinline__ uint32_t gemm_pack_bf16(float lo, float hi) {
-    gemm_f32x2 v = {lo, hi};
-    gemm_bf16x2 r = __builtin_convertvector(v, gemm_bf16x2);
-    uint32_t u;
-    __builtin_memcpy(&u, &r, 4);
-    return u;
-}
 
 // The codes and block constants in the order the products read them, made once per matrix: per tile of 32 rows and
 // chunk of 64 columns GEMM_TILE_BYTES consecutive bytes - one 16-byte word of codes per lane (row = lane % 32 of the

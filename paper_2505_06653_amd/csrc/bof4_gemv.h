@@ -98,6 +98,10 @@ __global__ __launch_bounds__(64 * GEMV_MAX_WAVES, T <= 2 ? 4 : T == 3 ? 3 : 2) v
     const uint32_t r1 = min(rows, r0 + rc);
     __syncthreads();
     const char* tab = reinterpret_cast<const char*>(sh.tab);
+    // (a layer's bias, factors and residuals are on their way while the rows are summed up)
+    typename Out::template Ahead<T> ahead = {};
+    if constexpr (Out::LAYER)
+        if (wave == 0 && lane < r1 - r0) ahead = out.template ask<T>(r0 + lane);
 
     for (uint32_t strip = wave; strip < n_strips; strip += n_waves) {
     const uint32_t col0 = strip * GEMV_STRIP + lane * 32;
@@ -245,7 +249,7 @@ __global__ __launch_bounds__(64 * GEMV_MAX_WAVES, T <= 2 ? 4 : T == 3 ? 3 : 2) v
         for (int t = 0; t < T; ++t) {
             float s = 0.0f;
             for (uint32_t p = 0; p < n_waves; ++p) s += sh.part[(p * rc + lane) * T + t];  // waves in order
-            if constexpr (Out::LAYER) out.template store<1>(t, r0 + lane, rows, &s);
+            if constexpr (Out::LAYER) out.template store_one<T>(t, r0 + lane, ahead, s);
             else out.first[(uint64_t)t * rows + r0 + lane] = s;
         }
     }

@@ -25,7 +25,7 @@ struct LinearGradArgs {
     uint64_t ld_dy, ld_pre, ld_mul, ld_dmul;
     uint32_t act;
     bool dy_bf16, pre_bf16, mul_bf16, dmul_bf16;
-    bool wide;  // four neighbouring elements of every tensor are aligned to their size
+    bool wide;  // eight neighbouring elements of every tensor begin on 16 bytes
 };
 
 // dz in the products' order (gemm_pack_x_kernel's, rows in the place of columns): a workgroup takes a chunk of 64 rows and
@@ -42,30 +42,25 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(LinearGradArgs a, uint32
     for (uint32_t tile = blockIdx.y * tiles_per_range; tile < tile1; ++tile) {
         const uint64_t t = tile * GEMM_TOKENS + token_in_tile;
         uint32_t w[4] = {0u, 0u, 0u, 0u};
-        if (t < n_tokens) {
+        if (t < n_tokens && row < rows) {
+            const uint32_t n = rows - row;
+            const bool whole = a.wide && n >= 8;
+            float dy[8], z[8] = {}, f[8], value, slope;
+            load_row<8>(a.dy, t * a.ld_dy + row, a.dy_bf16, whole, n, dy);
+            if (a.pre) load_row<8>(a.pre, t * a.ld_pre + row, a.pre_bf16, whole, n, z);
+            if (a.mul) load_row<8>(a.mul, t * a.ld_mul + row, a.mul_bf16, whole, n, f);
 #pragma unroll
-            for (uint32_t h = 0; h < 2; ++h) {
-                const uint32_t r = row + 4 * h;
-                if (r >= rows) break;
-                const uint32_t n = rows - r;
-                const bool whole = a.wide && n >= 4;
-                float dy[4], z[4] = {}, f[4], value[4], slope[4];
-                load_row<4>(a.dy, t * a.ld_dy + r, a.dy_bf16, whole, n, dy);
-                if (a.pre) load_row<4>(a.pre, t * a.ld_pre + r, a.pre_bf16, whole, n, z);
-                if (a.mul) load_row<4>(a.mul, t * a.ld_mul + r, a.mul_bf16, whole, n, f);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    activation_slope(a.act, z[i], value[i], slope[i]);
-                    value[i] *= dy[i];
-                    if (a.mul) dy[i] *= f[i];
-                    if (a.act != ACT_NONE) dy[i] *= slope[i];
-                    if ((uint32_t)i >= n) dy[i] = 0.0f;
-                    bias[4 * h + i] += dy[i];
-                }
-                if (a.dmul) store_row<4>(a.dmul, t * a.ld_dmul + r, a.dmul_bf16, whole, n, value);
-                w[2 * h] = gemm_pack_bf16(dy[0], dy[1]);
-                w[2 * h + 1] = gemm_pack_bf16(dy[2], dy[3]);
+            for (int i = 0; i < 8; ++i) {
+                activation_slope(a.act, z[i], value, slope);
+                z[i] = value * dy[i];
+                if (a.mul) dy[i] *= f[i];
+                if (a.act != ACT_NONE) dy[i] *= slope;
+                if ((uint32_t)i >= n) dy[i] = 0.0f;
+                bias[i] += dy[i];
             }
+            if (a.dmul) store_row<8>(a.dmul, t * a.ld_dmul + row, a.dmul_bf16, whole, n, z);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = gemm_pack_bf16(dy[2 * i], dy[2 * i + 1]);
         }
         xp[((uint64_t)tile * n_chunks + chunk) * GEMM_TILE_WORDS + (word & 3) * 64 + (word >> 2) * 32 + token_in_tile] =
             make_uint4(w[0], w[1], w[2], w[3]);

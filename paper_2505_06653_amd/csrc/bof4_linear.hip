@@ -25,7 +25,8 @@ struct Rows {
     uint32_t type;
     uint64_t ld;
     bool ok(uint64_t rows) const { return !p || (valid_type(type) && aligned(p, type_bytes(type)) && ld >= rows); }
-    bool wide() const { return !p || (aligned(p, 4 * type_bytes(type)) && ld % 4 == 0); }
+    bool wide() const { return !p || (aligned(p, 4 * type_bytes(type)) && ld % 4 == 0); }    // four elements in one access
+    bool wide8() const { return !p || (aligned(p, 16) && ld % (16 / type_bytes(type)) == 0); }  // eight, 16 bytes each
     // the other tensor of the same elements, or another place altogether
     bool same_or_apart(const Rows& o) const { return !p || p != o.p || (type == o.type && ld == o.ld); }
 };
@@ -64,8 +65,7 @@ LinearBackwardPlan backward_plan_one(uint64_t rows, uint64_t cols, uint64_t n_to
     const uint64_t tok_tiles = (n_tokens + GEMM_TOKENS - 1) / GEMM_TOKENS, row_chunks = (rows + GEMM_CHUNK - 1) / GEMM_CHUNK;
     LinearBackwardPlan P;
     P.turned = gemm_decoded_plan(cols, rows, tok_tiles);
-    uint64_t per = (tok_tiles + LINEAR_MOST_RANGES - 1) / LINEAR_MOST_RANGES;
-    if (per < 4) per = 4;
+    const uint64_t per = (tok_tiles + LINEAR_MOST_RANGES - 1) / LINEAR_MOST_RANGES;
     P.tiles_per_range = (uint32_t)per;
     P.ranges = (uint32_t)((tok_tiles + per - 1) / per);
     P.dbias = align_up(tok_tiles * GEMM_TOKENS * row_chunks * GEMM_CHUNK * 2, 256);
@@ -183,7 +183,7 @@ int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t co
     const LinearGradArgs a = {l.dy_dev, l.act != ACT_NONE || l.dmul_dev ? l.pre_dev : nullptr, l.mul_dev, l.dmul_dev,
                               l.dbias_dev ? dbias_parts : nullptr, l.ld_dy, l.ld_pre, l.ld_mul, l.ld_dmul, l.act,
                               l.dy_type == BOF4_BF16, l.pre_type == BOF4_BF16, l.mul_type == BOF4_BF16, l.dmul_type == BOF4_BF16,
-                              dy.wide() && pre.wide() && mul.wide() && dmul.wide()};
+                              dy.wide8() && pre.wide8() && mul.wide8() && dmul.wide8()};
     hipLaunchKernelGGL(linear_dz_kernel, dim3(row_chunks, P.ranges), dim3(256), 0, s, a, n_tokens, (uint32_t)rows, row_chunks,
                        tok_tiles, P.tiles_per_range, xp);
     if (l.dbias_dev)

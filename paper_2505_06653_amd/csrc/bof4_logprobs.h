@@ -529,7 +529,7 @@ __global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobsGradArgs a, 
         if constexpr (OUT_BF16) {
             uint32_t o[PER_WORD / 2];
 #pragma unroll
-            for (uint32_t i = 0; i < PER_WORD / 2; ++i) o[i] = f32_to_bf16_rne(d[2 * i]) | (f32_to_bf16_rne(d[2 * i + 1]) << 16);
+            for (uint32_t i = 0; i < PER_WORD / 2; ++i) o[i] = gemm_pack_bf16(d[2 * i], d[2 * i + 1]);
             if constexpr (PER_WORD == 8) store_stream(reinterpret_cast<uint4*>(to), make_uint4(o[0], o[1], o[2], o[3]));
             else *reinterpret_cast<uint2*>(to) = make_uint2(o[0], o[1]);
         } else {

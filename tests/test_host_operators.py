@@ -1,6 +1,9 @@
 """CPU-only checks of the layer operators' and the log probabilities' entry points: bad arguments are refused before any GPU
 call, sizes are host formulas."""
 import ctypes
+import os
+import re
+import struct
 
 import pytest
 
@@ -66,15 +69,34 @@ BAD_CB = CB[::-1].copy()
 BAD_CBP = BAD_CB.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
 
 
-def record(kind, **fields):
-    r = kind()
-    for k, v in fields.items():
-        setattr(r, k, v.value if isinstance(v, ctypes.c_void_p) else v)
-    return r
+LAYER = ("act", "bias_type", "mul_type", "residual_type", "y_type", "pre_type", "bias_dev", "mul_dev", "residual_dev", "y_dev",
+         "pre_dev", "ld_mul", "ld_residual", "ld_y", "ld_pre")
+GRADIENT = ("act", "dy_type", "pre_type", "mul_type", "dmul_type", "dx_type", "dy_dev", "pre_dev", "mul_dev", "dmul_dev",
+            "dbias_dev", "dx_dev", "ld_dy", "ld_pre", "ld_mul", "ld_dmul", "ld_dx")
+
+
+def record(packing, names, fields):
+    assert set(fields) <= set(names)
+    return packing.pack(*[fields.get(k) or 0 for k in names])
 
 
 def layer(**kw):
-    return record(binding.Layer, **{**dict(y_dev=0x40000, y_type=BF16, ld_y=64), **kw})
+    return record(binding.LAYER, LAYER, {**dict(y_dev=0x40000, y_type=BF16, ld_y=64), **kw})
+
+
+def test_packed_records_are_the_header_s_structs():
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "bof4.h")).read()
+    for name, names, packing in (("bof4_layer", LAYER, binding.LAYER), ("bof4_layer_gradient", GRADIENT, binding.LAYER_GRADIENT)):
+        body = re.sub(r"/\*.*?\*/", "", text[:text.index("} " + name + ";")].rsplit("typedef struct {", 1)[1], flags=re.S)
+        fields, kinds = [], ""
+        for line in body.split(";"):
+            if line.strip():
+                words = line.replace("*", " * ").split()
+                declared = [w.strip(",") for w in words if w.strip(",").endswith(("_dev", "_type")) or w.startswith("ld_") or w == "act"]
+                fields += declared
+                kinds += ("P" if "*" in words else "I" if "uint32_t" in words else "Q") * len(declared)
+        assert tuple(fields) == names
+        assert struct.Struct("@" + kinds).size == packing.size and kinds == "".join(int(n or 1) * k for n, k in re.findall(r"(\d*)([IPQ])", packing.format))
 
 
 def gemv_linear(codes=P, scales=P, rows=64, cols=128, block=64, cb=CBP, table=None, k=0, x=at(0x20000), n=2, lay=None, null=False, **kw):
@@ -114,7 +136,8 @@ def test_gemm_linear_refuses(bad):
 
 
 def gemm_linear_backward(packed=P, rows=64, cols=128, cb=CBP, table=None, k=0, n=2, ws=at(0x80000), size=1 << 40, null=False, **kw):
-    g = record(binding.LayerGradient, **{**dict(dy_dev=0x20000, dy_type=BF16, ld_dy=64, dx_dev=0x40000, dx_type=BF16, ld_dx=128), **kw})
+    g = record(binding.LAYER_GRADIENT, GRADIENT,
+               {**dict(dy_dev=0x20000, dy_type=BF16, ld_dy=64, dx_dev=0x40000, dx_type=BF16, ld_dx=128), **kw})
     return binding.lib().bof4_gemm_linear_backward(packed, rows, cols, cb, table, k, n, None if null else g, ws, size, None)
 
 
