@@ -378,8 +378,9 @@ size_t bof4_gemm_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t n_tokens
  * A linear layer around the products with a quantised matrix, in one call and without the product on its way through memory:
  *     z = x W^T + bias,   y = act(z) * mul + residual
  * with W and its list as bof4_gemv (bof4_gemv_linear: one token to a few) or bof4_gemm (bof4_gemm_linear: 8 or more) takes
- * them, and the sums as those make them (their order and errors are stated there).  Everything behind the sums is binary32; each
- * tensor written is rounded once.  The gate of a gated layer is mul: with u = x Wu^T, silu(x Wg^T) * u.
+ * them, and the sums within the bounds that are stated there (bof4_gemm_linear's are those of bof4_gemm bit for bit where y or
+ * pre is binary32; where all that is written is bfloat16 its chains of additions are cut less).  Everything behind the sums is
+ * binary32; each tensor written is rounded once.  The gate of a gated layer is mul: with u = x Wu^T, silu(x Wg^T) * u.
  */
 #define BOF4_ACT_NONE 0u
 #define BOF4_ACT_RELU 1u
@@ -472,7 +473,7 @@ size_t bof4_token_logprobs_workspace_bytes(uint64_t n_rows, uint64_t vocab, uint
  *   d_logits_dev  n_rows x vocab of d_logits_type, row stride ld_d_logits (>= vocab), all of it written; may be the logits
  *               themselves (one type and one row stride)
  * A logit of -inf and a row of nothing else have a gradient of 0 (the target's own part g aside); a row with a NaN or +inf
- * has NaN.  Limits as above, and fewer than 2^24 stretches of 4096 (binary32) or 8192 (bfloat16) logits.  Only enqueues.
+ * has NaN.  Limits as above, and fewer than 2^24 stretches of 2048 logits.  Only enqueues.
  */
 int bof4_token_logprobs_backward(const void* logits_dev, uint32_t logits_type, uint64_t n_rows, uint64_t vocab,
                                  uint64_t ld_logits, const float* stats_dev, const int64_t* target_dev,

@@ -311,4 +311,14 @@ inline GemmPlan gemm_plan(uint64_t rows, uint64_t cols, uint64_t n_tokens, bool 
     return P;
 }
 
+// A layer whose results are all rounded to bfloat16 needs none of what keeps the last bits of the sums: chains of 512 columns
+// in the 256 x 128 tile, uncut ones in gemm_kernel.  Their error, some 10^-7 of the sums, is below a ten-thousandth of the
+// results' rounding.  With a list: 11008 x 4096, 500 tokens, the product 87 -> 73 us.
+inline void gemm_plan_for_bf16(GemmPlan& P) {
+    P.chains.list_flush = 0xffffffffu;
+    P.chains.n_runs = 1;
+    P.chains.wide_flush = P.decoded.flush = 8;
+    P.chains.wide_carry = P.decoded.carry = false;
+}
+
 }  // namespace bof4

@@ -455,16 +455,20 @@ struct LogprobsGradArgs {
     const int64_t* target;
     const float *stats, *d_logprob, *entropy, *d_entropy;
 };
-constexpr uint32_t LOGPROBS_GRAD_WORDS = 4;  // 16-byte words per thread
+// Eight logits per thread: one word of bfloat16, two of binary32 (2000 x 32000, one / two / four words: bfloat16 42 / 45 / 49 us,
+// binary32 to bfloat16 67 / 65 / 66).
+constexpr uint32_t logprobs_grad_words(bool bf16) { return bf16 ? 1 : 2; }
+constexpr uint32_t LOGPROBS_GRAD_STRETCH = 256 * 8;  // logits per workgroup
 template <bool BF16, bool OUT_BF16, bool ENTROPY>
 __global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobsGradArgs a, uint32_t stretches) {
     constexpr uint32_t PER_WORD = logprobs_word_elements(BF16), SIZE = BF16 ? 2 : 4, OUT_SIZE = OUT_BF16 ? 2 : 4;
+    constexpr uint32_t WORDS = logprobs_grad_words(BF16);
     const uint32_t row = blockIdx.x / stretches, stretch = blockIdx.x - row * stretches;
     const char* row_ptr = static_cast<const char*>(a.logits) + (uint64_t)row * a.ld * SIZE;
     const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(row_ptr) & 15u) / SIZE;
     const char* words = row_ptr - off * SIZE;
     const uint32_t end = off + a.vocab, n_words = (end + PER_WORD - 1) / PER_WORD;
-    const uint32_t w0 = stretch * 256 * LOGPROBS_GRAD_WORDS + threadIdx.x;
+    const uint32_t w0 = stretch * 256 * WORDS + threadIdx.x;
     char* out = static_cast<char*>(a.out) + (uint64_t)row * a.ld_out * OUT_SIZE - (uint64_t)off * OUT_SIZE;
     const bool wide = (reinterpret_cast<uintptr_t>(out) & (PER_WORD * OUT_SIZE < 16 ? PER_WORD * OUT_SIZE - 1 : 15u)) == 0u;
     const float m = a.stats[2 * (uint64_t)row], log_s = a.stats[2 * (uint64_t)row + 1];
@@ -487,16 +491,16 @@ __global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobsGradArgs a, 
         if constexpr (OUT_BF16) reinterpret_cast<uint16_t*>(out)[j] = (uint16_t)f32_to_bf16_rne(d);
         else reinterpret_cast<float*>(out)[j] = d;
     };
-    uint4 q[LOGPROBS_GRAD_WORDS];
-    bool whole[LOGPROBS_GRAD_WORDS];
+    uint4 q[WORDS];
+    bool whole[WORDS];
 #pragma unroll
-    for (uint32_t k = 0; k < LOGPROBS_GRAD_WORDS; ++k) {
+    for (uint32_t k = 0; k < WORDS; ++k) {
         const uint32_t w = w0 + 256 * k, first = w * PER_WORD;
         whole[k] = w < n_words && first >= off && first + PER_WORD <= end;
         if (whole[k]) q[k] = load_stream(reinterpret_cast<const uint4*>(words) + w);
     }
 #pragma unroll
-    for (uint32_t k = 0; k < LOGPROBS_GRAD_WORDS; ++k) {
+    for (uint32_t k = 0; k < WORDS; ++k) {
         const uint32_t w = w0 + 256 * k, first = w * PER_WORD;
         if (!whole[k]) {
             if (w < n_words)

@@ -114,9 +114,9 @@ int bof4_token_logprobs_backward(const void* logits_dev, uint32_t logits_type, u
                                 target_dev, stats_dev, d_logprob_dev, entropy_dev, d_entropy_dev};
     const bool bf16 = logits_type == BOF4_BF16;
     const uint64_t per_word = logprobs_word_elements(bf16), words = (vocab + 2 * per_word - 2) / per_word;  // wherever a row begins
-    const uint64_t stretches = (words + 256 * LOGPROBS_GRAD_WORDS - 1) / (256 * LOGPROBS_GRAD_WORDS);
+    const uint64_t stretches = (words * per_word + LOGPROBS_GRAD_STRETCH - 1) / LOGPROBS_GRAD_STRETCH;
     if (n_rows * stretches >= 1ull << 24)
-        return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: 2^24 and more stretches of 4096 (binary32) or 8192 logits");
+        return fail(BOF4_ERR_ARG, "bof4_token_logprobs_backward: 2^24 and more stretches of 2048 logits");
     const dim3 grid((uint32_t)(n_rows * stretches));
     timing_begin(s);
 #define BOF4_LAUNCH_GRAD(IN_, OUT_)                                                                                     \

@@ -188,7 +188,13 @@ int gemm_run(const GemmCall& call, const GemmPlan& P, Out dst) {
                        cb, offsets_dev, entries_dev, (uint32_t)n_outliers, T.lg, T.row_tiles,                       \
                        (uint32_t)gemm_row_tiles(rows), xp, tok_tiles, tok_groups, W.per_split, C.wide_flush, n_tokens,     \
                        W.split, dst);
-        if (n_outliers > 0) { BOF4_LAUNCH_WIDE(true, true) }
+        if (n_outliers > 0) {
+            if constexpr (Out::LAYER) {
+                if (C.wide_carry) { BOF4_LAUNCH_WIDE(true, true) } else { BOF4_LAUNCH_WIDE(true, false) }
+            } else {
+                BOF4_LAUNCH_WIDE(true, true)
+            }
+        }
         else if (C.wide_carry) { BOF4_LAUNCH_WIDE(false, true) }
         else { BOF4_LAUNCH_WIDE(false, false) }
 #undef BOF4_LAUNCH_WIDE
