@@ -848,16 +848,32 @@ __global__ __launch_bounds__(64 * GEMM_DECODE_WAVES) void gemm_decode_kernel(
     }
 }
 
-// The product over the decoded tiles, with the tile and the steps of gemm_wide_kernel: 256 rows x 128 tokens per
-// workgroup of eight waves, one chunk of 64 columns per step, three LDS buffers, each wave bringing in one row tile of the
-// chunk after the next and its share of x, the quarter's LDS reads under way while the one before is multiplied.  The same
-// additions in the same order: where the columns are split alike, the results are gemm_wide_kernel's bit for bit.
-//   What bounds it: of a chunk's 2150 clocks the matrix cores are busy 1024, the LDS unit 912, the vector units 767 (12288 x
-// 4096, 2000 tokens, with a list, at the 1.81 GHz that the card holds meanwhile); 1.04 to 1.19 PFLOP/s, where a large product
-// of the library reaches 1.17 to 1.22.  One product per two LDS reads in the order of issue: 2 to 3 % faster than four products
-// after four reads; the waves' priority raised for the products 4 to 8 % slower; the tiles' sums carried in turns no difference.
-//   2000 tokens with a list, gemm_wide_kernel -> decoding and this: 4096 x 4096 127 -> 102 us, 12288 x 4096 353 -> 252, 22016 x
-// 4096 649 -> 482, 8192 x 28672 1305 -> 1042.
+// The product over the decoded tiles, with the tile of gemm_wide_kernel: 256 rows x 128 tokens per workgroup of eight waves,
+// one chunk of 64 columns per step in quarters of one 16-byte word of every operand, three LDS buffers.  The same additions in
+// the same order: where the columns are split alike, the results are gemm_wide_kernel's bit for bit.
+//   Operands go from memory to LDS without passing through registers (the tiles lie in memory as they lie in LDS: a wave's
+// request is 1024 bytes on either side), one row tile and a share of x per wave and chunk.  A step's one barrier stands in
+// front of its last quarter: by then every wave has its last words of the step's buffer in registers, so chunk s + 3 may come
+// into it, and has waited for its own share of chunk s + 1 (six requests; the six of chunk s + 2 stay on their way), so the
+// last quarter can already ask for the next step's first words.  A request has two steps' time.
+//   What bounds it: the matrix cores' rate at the clock that the card holds meanwhile (1.8 GHz); 1.1 to 1.2 PFLOP/s, where a large
+// product of the library reaches 1.17 to 1.22.  One product per two LDS reads in the order of issue: 2 to 3 % faster than four
+// products after four reads; the waves' priority raised for the products 4 to 8 % slower; the tiles' sums carried in turns no
+// difference.  Against bringing the operands in through registers, gradient calls whole, 11008 x 4096 with 2000 tokens 226 ->
+// 213 us, 4096 x 11008 248 -> 232, 22016 x 4096 with 4096 828 -> 782; with the barrier at the step's end, where a request has one
+// step, 219 -> 206 on one card and 800 -> 885 on the largest; 128 x 128 tiles in four waves, two workgroups a compute unit, 248.
+//   2000 tokens with a list, gemm_wide_kernel -> decoding and this (through registers): 4096 x 4096 127 -> 102 us, 12288 x 4096
+// 353 -> 252, 22016 x 4096 649 -> 482, 8192 x 28672 1305 -> 1042.
+constexpr int GEMM_WAIT_ALL_LDS = 0x0f70;        // s_waitcnt: no request on its way into LDS
+constexpr int GEMM_WAIT_BUT_6_AND_READS = 0x0076;  // all requests but the last six, and every LDS read
+constexpr int GEMM_WAIT_BUT_12 = 0x0f7c;
+// A barrier that waits for nothing by itself; no memory access moves across it.
+__device__ __forceinline__ void gemm_bare_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 template <bool CARRY, class Out>
 __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
     const uint4* __restrict__ decoded, uint32_t first_row, uint32_t n_rt, uint32_t rows, uint32_t n_chunks,
@@ -883,20 +899,16 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
     const uint4* my_a = decoded + (uint64_t)min(rg * GEMM_WIDE_WAVES + wave, n_rt - 1) * n_chunks * GEMM_TILE_WORDS + lane;
     const uint4* my_x = xp + (uint64_t)min(tg * GEMM_WIDE_TOK_TILES + (wave >> 1), tok_tiles - 1) * n_chunks * GEMM_TILE_WORDS +
                         (wave & 1) * 128 + lane;
-    struct Ahead {  // what a wave brings into LDS for one chunk
-        uint4 a0, a1, a2, a3, x0, x1;
-    };
-    auto fetch = [&](uint32_t nth) __attribute__((always_inline)) {
+    // The wave's share of a chunk, six requests; past the last chunk the last one again, so that there are always six.
+    auto bring = [&](uint32_t nth, uint32_t buf) __attribute__((always_inline)) {
         const uint64_t at = (uint64_t)min(ch0 + nth, ch1 - 1) * GEMM_TILE_WORDS;
-        const uint4 *a = my_a + at, *x = my_x + at;
-        Ahead o;
-        o.a0 = a[0];
-        o.a1 = a[64];
-        o.a2 = a[128];
-        o.a3 = a[192];
-        o.x0 = x[0];
-        o.x1 = x[64];
-        return o;
+        typedef const __attribute__((address_space(1))) void* G;
+        typedef __attribute__((address_space(3))) void* L;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) __builtin_amdgcn_global_load_lds((G)(my_a + at + 64 * j), (L)&sh.a[buf][wave][64 * j], 16, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            __builtin_amdgcn_global_load_lds((G)(my_x + at + 64 * j), (L)&sh.b[buf][wave >> 1][(wave & 1) * 128 + 64 * j], 16, 0, 0);
     };
     gemm_f32x16 acc[2][2], sum[2][2];  // [row tile][token tile]
 #pragma unroll
@@ -915,33 +927,30 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
         const Operands o = {{a[64 * j], a[GEMM_TILE_WORDS + 64 * j]}, {b[64 * j], b[GEMM_TILE_WORDS + 64 * j]}};
         return o;
     };
-    auto store_quarter = [&](const Ahead o, uint32_t buf, int j) __attribute__((always_inline)) {
-        sh.a[buf][wave][64 * j + lane] = j == 0 ? o.a0 : j == 1 ? o.a1 : j == 2 ? o.a2 : o.a3;
-        if (j >= 2) sh.b[buf][wave >> 1][(wave & 1) * 128 + 64 * (j - 2) + lane] = j == 2 ? o.x0 : o.x1;
-    };
     uint32_t until_flush = flush;
-    // Before step s: buffer s % 3 holds chunk s and buffer (s + 1) % 3 chunk s + 1; `o` is chunk s + 2, on its way since the
-    // step before; chunk s + 3 is asked for during the step; `op` are the operands of the step's first quarter.
+    // Before step s: chunk s is in buffer s % 3, chunks s + 1 and s + 2 are on their way into the next two; `op` are the operands
+    // of the step's first quarter.
     Operands op;
-    auto step = [&](uint32_t s, const uint32_t buf, const Ahead o) __attribute__((always_inline)) {
-        const uint32_t buf1 = buf == 2u ? 0u : buf + 1u, buf2 = buf == 0u ? 2u : buf - 1u;
-        const Ahead asked = fetch(s + 3);
+    auto step = [&](uint32_t s, const uint32_t buf) __attribute__((always_inline)) {
+        const uint32_t buf1 = buf == 2u ? 0u : buf + 1u;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+            if (j == 3) {
+                __builtin_amdgcn_s_waitcnt(GEMM_WAIT_BUT_6_AND_READS);
+                gemm_bare_barrier();
+                bring(s + 3, buf);
+            }
             const Operands next = read_operands(j < 3 ? buf : buf1, (j + 1) & 3);
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
                     acc[r][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.b[t], op.a[r], acc[r][t], 0, 0, 0);
-            store_quarter(o, buf2, j);
             __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
             __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x200, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
             __builtin_amdgcn_sched_barrier(0);
             op = next;
         }
@@ -961,45 +970,24 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
                         }
                     }
         }
-        __syncthreads();
-        return asked;
     };
-    Ahead o0;
-    {
-        const Ahead first = fetch(0), second = fetch(1);
-        o0 = fetch(2);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            store_quarter(first, 0, j);
-            store_quarter(second, 1, j);
-        }
-        __syncthreads();
-        op = read_operands(0, 0);
-    }
-    // Six steps to a round, so that neither the buffers' places nor the registers of what is on its way move (a copy of a
-    // register that is being loaded waits for the load).
-    uint32_t s = 0;
-    for (uint32_t rounds = n_steps / 6; rounds > 0; --rounds, s += 6) {
-        const Ahead o1 = step(s, 0, o0);
-        const Ahead o2 = step(s + 1, 1, o1);
-        const Ahead o3 = step(s + 2, 2, o2);
-        const Ahead o4 = step(s + 3, 0, o3);
-        const Ahead o5 = step(s + 4, 1, o4);
-        o0 = step(s + 5, 2, o5);
+    bring(0, 0);
+    bring(1, 1);
+    bring(2, 2);
+    __builtin_amdgcn_s_waitcnt(GEMM_WAIT_BUT_12);
+    gemm_bare_barrier();
+    op = read_operands(0, 0);
+    uint32_t s = 0;  // (three steps to a round, so that the buffers' places do not move)
+    for (uint32_t rounds = n_steps / 3; rounds > 0; --rounds, s += 3) {
+        step(s, 0);
+        step(s + 1, 1);
+        step(s + 2, 2);
     }
     if (s < n_steps) {
-        const Ahead o1 = step(s, 0, o0);
-        if (s + 1 < n_steps) {
-            const Ahead o2 = step(s + 1, 1, o1);
-            if (s + 2 < n_steps) {
-                const Ahead o3 = step(s + 2, 2, o2);
-                if (s + 3 < n_steps) {
-                    const Ahead o4 = step(s + 3, 0, o3);
-                    if (s + 4 < n_steps) step(s + 4, 1, o4);
-                }
-            }
-        }
+        step(s, 0);
+        if (s + 1 < n_steps) step(s + 1, 1);
     }
+    __builtin_amdgcn_s_waitcnt(GEMM_WAIT_ALL_LDS);  // (chunks past the last were asked for, too)
     if constexpr (Out::LAYER) {
         if (n_parts == 1) {
             gemm_store_tiles(dst, &sh.a[0][0][0], wave, lane, sum, acc, first_row + (rg * GEMM_WIDE_WAVES + wr) * GEMM_ROWS,
@@ -1024,6 +1012,7 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
         }
     }
 }
+
 
 // y = the partial results in order (count elements each): the first, which may stand in y itself, and n_more others.
 static __global__ __launch_bounds__(256) void gemm_sum_kernel(const float* first, const float* __restrict__ more, uint32_t n_more,
