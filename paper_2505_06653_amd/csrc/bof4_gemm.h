@@ -65,10 +65,9 @@ static __global__ __launch_bounds__(256) void gemm_pack_weights_kernel(const uin
 // x in the order the products read it, made once per call: for every tile of 32 tokens, chunk of 64 columns and
 // product j one 16-byte word per lane (token = lane % 32 of the tile, columns 32 (lane / 32) + 8 j .. + 7 of the
 // chunk), so that a wave's load is 1 KiB of consecutive memory; zeros past the last token and the last column.
-static __global__ __launch_bounds__(256) void gemm_pack_x_kernel(const uint16_t* __restrict__ x, uint32_t n_tokens,
-                                                          uint32_t cols, uint32_t n_chunks, uint32_t n_pad,
-                                                          uint4* __restrict__ xp) {
-    const uint64_t idx = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+__device__ __forceinline__ void gemm_pack_x(uint32_t block, const uint16_t* __restrict__ x, uint32_t n_tokens, uint32_t cols,
+                                            uint32_t n_chunks, uint32_t n_pad, uint4* __restrict__ xp) {
+    const uint64_t idx = (uint64_t)block * 256 + threadIdx.x;
     const uint64_t total = (uint64_t)(n_pad / 32) * n_chunks * 256;
     if (idx >= total) return;
     const uint32_t lane = (uint32_t)(idx & 63), j = (uint32_t)((idx >> 6) & 3);
@@ -78,6 +77,19 @@ static __global__ __launch_bounds__(256) void gemm_pack_x_kernel(const uint16_t*
     uint4 v = make_uint4(0u, 0u, 0u, 0u);
     if (n < n_tokens && c < cols) v = *reinterpret_cast<const uint4*>(x + (uint64_t)n * cols + c);
     xp[idx] = v;
+}
+static __global__ __launch_bounds__(256) void gemm_pack_x_kernel(const uint16_t* __restrict__ x, uint32_t n_tokens,
+                                                                 uint32_t cols, uint32_t n_chunks, uint32_t n_pad,
+                                                                 uint4* __restrict__ xp) {
+    gemm_pack_x(blockIdx.x, x, n_tokens, cols, n_chunks, n_pad, xp);
+}
+// Two kinds of workgroups in one launch, n_first of the first kind dealt out evenly among `total`, so that both are under way
+// all the time: is workgroup `id` of the first kind, and the how-many-th of its kind is it.
+__device__ __forceinline__ bool gemm_deal(uint32_t& id, uint32_t n_first, uint32_t total) {
+    const uint32_t before = (uint32_t)((uint64_t)id * n_first / total);
+    const bool first = (uint32_t)((uint64_t)(id + 1) * n_first / total) > before;
+    id = first ? before : id - before;
+    return first;
 }
 
 // The outlier list in the order of the products' tiles, made once per matrix.  ptr[rt * n_groups + g] is where the
@@ -763,26 +775,33 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_wide_kernel(
 // Many more tokens: the matrix is decoded once, to bfloat16 in the order of the products' operands (gemm_decode_kernel, a
 // 4096-byte tile per 32 rows and 64 columns, list entries in place), and multiplied by gemm_decoded_kernel, which has
 // nothing to decode.  gemm_wide_kernel decodes a weight once per 128 tokens.
-// One wave per GEMM_DECODE_TILES tiles of one row tile, all of whose codes are on their way at once.  Bound by memory: 50 M
+// One wave per GEMM_DECODE_TILES tiles of one row tile, all of whose codes are on their way at once; the first launch of a call
+// reorders x as well (pack_groups workgroups, gemm_pack_x).  Bound by memory: 50 M
 // weights in 23 us (5.7 TB/s) where what it writes stays in the 256 MB cache behind the L2s, half of that beyond.
 constexpr uint32_t GEMM_DECODE_TILES = 4, GEMM_DECODE_WAVES = 4;
 template <bool OUTLIERS>
 __global__ __launch_bounds__(64 * GEMM_DECODE_WAVES) void gemm_decode_kernel(
     const char* __restrict__ packed, uint32_t first_rt, uint32_t n_rt, uint32_t n_chunks, CodebookArgs cb,
     const uint32_t* __restrict__ list_ptr, const uint32_t* __restrict__ entries, uint32_t n_out, GemmListGeometry lg,
-    uint32_t row_tiles, uint4* __restrict__ decoded) {
+    uint32_t row_tiles, uint4* __restrict__ decoded, uint32_t pack_groups, const uint16_t* __restrict__ x, uint32_t n_tokens,
+    uint32_t cols, uint32_t n_pad, uint4* __restrict__ xp) {
     struct Shared {
         float tab[16];
         uint4 parked[OUTLIERS ? GEMM_DECODE_WAVES : 1][OUTLIERS ? 4 * 64 : 1];
     };
     __shared__ __attribute__((aligned(16))) Shared sh;
+    uint32_t group = blockIdx.x;
+    if (gemm_deal(group, pack_groups, gridDim.x)) {
+        gemm_pack_x(group, x, n_tokens, cols, n_chunks, n_pad, xp);
+        return;
+    }
     const uint32_t tid = threadIdx.x, lane = tid & 63;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (tid < 16) sh.tab[tid] = cb.lv32[tid];
     __syncthreads();
     const char* tab = reinterpret_cast<const char*>(sh.tab);
     const uint32_t runs = (n_chunks + GEMM_DECODE_TILES - 1) / GEMM_DECODE_TILES;
-    const uint64_t job = (uint64_t)blockIdx.x * GEMM_DECODE_WAVES + wave;
+    const uint64_t job = (uint64_t)group * GEMM_DECODE_WAVES + wave;
     if (job >= (uint64_t)n_rt * runs) return;
     const uint32_t rt_local = (uint32_t)(job / runs), ch0 = (uint32_t)(job % runs) * GEMM_DECODE_TILES;
     const uint32_t n = min(GEMM_DECODE_TILES, n_chunks - ch0), rt = first_rt + rt_local;
@@ -1026,25 +1045,31 @@ static __global__ __launch_bounds__(256) void gemm_sum_kernel(const float* first
 
 
 // A layer's result from the partial sums in order (n_parts of n_tokens x rows each).  A workgroup takes 1024 rows, four to a
-// lane, of the tokens blockIdx.y, + gridDim.y, ...
+// lane, of the tokens `first`, + step, ...
 template <class Out>
-__global__ __launch_bounds__(256) void gemm_sum_layer_kernel(uint32_t n_parts, uint32_t n_tokens, uint32_t rows, Out dst) {
-    const uint32_t row = (blockIdx.x * 256 + threadIdx.x) * 4;
+__device__ __forceinline__ void gemm_sum_layer(uint32_t group, uint32_t first, uint32_t step, uint32_t n_parts, uint32_t n_tokens,
+                                               uint32_t rows, const Out& dst) {
+    const uint32_t row = (group * 256 + threadIdx.x) * 4;
     if (row >= rows) return;
     const uint64_t count = (uint64_t)n_tokens * rows;
-    for (uint32_t token = blockIdx.y; token < n_tokens; token += gridDim.y) {
+    for (uint32_t token = first; token < n_tokens; token += step) {
         const float* p = dst.parts + (uint64_t)token * rows + row;
         const bool whole = row + 4 <= rows && (rows & 3u) == 0u;
         double s[4] = {0.0, 0.0, 0.0, 0.0};
-        for (uint32_t k = 0; k < n_parts; ++k, p += count) {
+#pragma unroll 4
+        for (uint32_t k = 0; k < n_parts; ++k) {
             float v[4];
-            load_row<4>(p, 0, false, whole, rows - row, v);
+            load_row<4>(p + k * count, 0, false, whole, rows - row, v);
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[i] += v[i];
         }
         const float sums[4] = {(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
         dst.template store<4>(token, row, rows, sums);
     }
+}
+template <class Out>
+__global__ __launch_bounds__(256) void gemm_sum_layer_kernel(uint32_t n_parts, uint32_t n_tokens, uint32_t rows, Out dst) {
+    gemm_sum_layer(blockIdx.x, blockIdx.y, gridDim.y, n_parts, n_tokens, rows, dst);
 }
 
 }  // namespace bof4

@@ -6,7 +6,7 @@
 // tokens does whose matrix is decoded first: linear_turn_kernel decodes the packed matrix into the operands of W^^T, in
 // slabs that stay in the cache behind the L2s, and gemm_decoded_kernel multiplies them with dz.  dz is rounded to bfloat16
 // once, which is what the matrix cores take: each term is off by 2^-9 of itself at most, as far as dx's own rounding to
-// bfloat16 (without activation and factor dz is dy, and nothing is rounded).  linear_dz_kernel makes it from dy in the
+// bfloat16 (without activation and factor dz is dy, and nothing is rounded).  linear_dz makes it from dy in the
 // order of the operands, and dmul and dbias on the way.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -30,16 +30,18 @@ struct LinearGradArgs {
 
 // dz in the products' order (gemm_pack_x_kernel's, rows in the place of columns): a workgroup takes a chunk of 64 rows and
 // `tiles_per_range` tiles of 32 tokens, eight threads per token, which read 128 consecutive bytes and write 16-byte words of
-// which eight neighbouring tokens make up 128.  Bound by memory: 2000 tokens x 11008 rows with factor, activation and dmul.
+// which eight neighbouring tokens make up 128.  Bound by memory: 2000 tokens x 11008 rows with factor, activation and dmul, 220
+// MB, 44 us (5.0 TB/s; with 8-byte accesses 55).
 constexpr uint32_t LINEAR_MOST_RANGES = 64;  // parts of dbias at most
-__global__ __launch_bounds__(256) void linear_dz_kernel(LinearGradArgs a, uint32_t n_tokens, uint32_t rows, uint32_t n_chunks,
-                                                        uint32_t tok_tiles, uint32_t tiles_per_range, uint4* __restrict__ xp) {
-    __shared__ float sums[32][65];
-    const uint32_t tid = threadIdx.x, word = tid & 7, token_in_tile = tid >> 3, chunk = blockIdx.x;
+typedef float LinearDzSums[32][65];
+__device__ __forceinline__ void linear_dz(uint32_t chunk, uint32_t range, LinearDzSums& sums, const LinearGradArgs& a,
+                                          uint32_t n_tokens, uint32_t rows, uint32_t n_chunks, uint32_t tok_tiles,
+                                          uint32_t tiles_per_range, uint4* __restrict__ xp) {
+    const uint32_t tid = threadIdx.x, word = tid & 7, token_in_tile = tid >> 3;
     const uint32_t row = chunk * GEMM_CHUNK + 8 * word;
     float bias[8] = {};
-    const uint32_t tile1 = min(tok_tiles, (blockIdx.y + 1) * tiles_per_range);
-    for (uint32_t tile = blockIdx.y * tiles_per_range; tile < tile1; ++tile) {
+    const uint32_t tile1 = min(tok_tiles, (range + 1) * tiles_per_range);
+    for (uint32_t tile = range * tiles_per_range; tile < tile1; ++tile) {
         const uint64_t t = tile * GEMM_TOKENS + token_in_tile;
         uint32_t w[4] = {0u, 0u, 0u, 0u};
         if (t < n_tokens && row < rows) {
@@ -72,40 +74,70 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(LinearGradArgs a, uint32
     if (tid < GEMM_CHUNK && chunk * GEMM_CHUNK + tid < rows) {
         float s = 0.0f;
         for (uint32_t k = 0; k < 32; ++k) s += sums[k][tid];
-        a.dbias_parts[(uint64_t)blockIdx.y * rows + chunk * GEMM_CHUNK + tid] = s;
+        a.dbias_parts[(uint64_t)range * rows + chunk * GEMM_CHUNK + tid] = s;
     }
+}
+__device__ __forceinline__ void linear_dbias(uint32_t group, const float* __restrict__ parts, uint32_t n_parts, uint32_t rows,
+                                             float* __restrict__ dbias) {
+    const uint32_t row = group * 256 + threadIdx.x;
+    if (row >= rows) return;
+    double s = 0.0;
+#pragma unroll 8
+    for (uint32_t k = 0; k < n_parts; ++k) s += parts[(uint64_t)k * rows + row];
+    dbias[row] = (float)s;
 }
 __global__ __launch_bounds__(256) void linear_dbias_kernel(const float* __restrict__ parts, uint32_t n_parts, uint32_t rows,
                                                            float* __restrict__ dbias) {
-    const uint32_t row = blockIdx.x * 256 + threadIdx.x;
-    if (row >= rows) return;
-    double s = 0.0;
-    for (uint32_t k = 0; k < n_parts; ++k) s += parts[(uint64_t)k * rows + row];
-    dbias[row] = (float)s;
+    linear_dbias(blockIdx.x, parts, n_parts, rows, dbias);
+}
+
+__global__ __launch_bounds__(256) void linear_dz_kernel(LinearGradArgs a, uint32_t n_tokens, uint32_t rows, uint32_t n_chunks,
+                                                        uint32_t tok_tiles, uint32_t tiles_per_range, uint4* __restrict__ xp) {
+    __shared__ LinearDzSums sums;
+    linear_dz(blockIdx.x, blockIdx.y, sums, a, n_tokens, rows, n_chunks, tok_tiles, tiles_per_range, xp);
 }
 
 // W^^T in the order of the operands: 4096-byte tiles of 32 columns x 64 rows, from the packed tiles of 32 rows x 64 columns.
 // A wave turns 64 rows x 64 columns: it decodes as gemm_decode_kernel does (lane = row, 32 columns), puts neighbouring rows
 // of a column together with its neighbour lane (one lane exchange and one byte permutation per two weights), parks the
 // pairs in LDS by column, writes the tiles' list entries over their placeholders there and reads eight rows of a column at
-// a time.  A column takes LINEAR_TURN_LD bytes, so that sixteen lanes' 16-byte reads fall into different banks.
+// a time.  A column takes LINEAR_TURN_LD bytes, so that sixteen lanes' 16-byte reads fall into different banks.  Bound by the
+// look-ups and LDS traffic next to memory: 45 M weights in 24 us with a list, 16 M in 8 us without (gemm_decode_kernel, which turns
+// nothing, 19.5 and 7).
 constexpr uint32_t LINEAR_TURN_WAVES = 4, LINEAR_TURN_LD = 144;
+//   For small dz the first launch of a call makes it as well: dz_groups workgroups, dealt out among the others, so that the one's memory
+// accesses and the other's look-ups and LDS traffic overlap.
+struct LinearDzCall {
+    LinearGradArgs a;
+    uint32_t dz_groups, n_tokens, rows, tok_tiles, tiles_per_range;
+    uint4* xp;
+};
 template <bool OUTLIERS>
 __global__ __launch_bounds__(64 * LINEAR_TURN_WAVES) void linear_turn_kernel(
     const char* __restrict__ packed, uint32_t first_ct, uint32_t n_ct, uint32_t n_chunks, uint32_t row_chunks, CodebookArgs cb,
     const uint32_t* __restrict__ list_ptr, const uint32_t* __restrict__ entries, uint32_t n_out, GemmListGeometry lg,
-    uint32_t row_tiles, uint4* __restrict__ decoded) {
-    struct Shared {
+    uint32_t row_tiles, uint4* __restrict__ decoded, LinearDzCall dz) {
+    struct Turn {
         float tab[16];
         uint4 turned[LINEAR_TURN_WAVES][64 * LINEAR_TURN_LD / 16];
     };
-    __shared__ __attribute__((aligned(16))) Shared sh;
+    __shared__ __attribute__((aligned(16))) union {
+        Turn turn;
+        LinearDzSums sums;
+    } shared;
+    uint32_t group = blockIdx.x;
+    if (gemm_deal(group, dz.dz_groups, gridDim.x)) {
+        linear_dz(group % row_chunks, group / row_chunks, shared.sums, dz.a, dz.n_tokens, dz.rows, row_chunks, dz.tok_tiles,
+                  dz.tiles_per_range, dz.xp);
+        return;
+    }
+    Turn& sh = shared.turn;
     const uint32_t tid = threadIdx.x, lane = tid & 63;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (tid < 16) sh.tab[tid] = cb.lv32[tid];
     __syncthreads();
     const char* tab = reinterpret_cast<const char*>(sh.tab);
-    const uint64_t job = (uint64_t)blockIdx.x * LINEAR_TURN_WAVES + wave;
+    const uint64_t job = (uint64_t)group * LINEAR_TURN_WAVES + wave;
     if (job >= (uint64_t)((n_ct + 1) / 2) * row_chunks) return;
     const uint32_t ct_local = 2 * (uint32_t)(job / row_chunks), rc = (uint32_t)(job % row_chunks);
     const uint32_t ch = (first_ct + ct_local) / 2;  // (first_ct is even)
@@ -171,6 +203,15 @@ __global__ __launch_bounds__(64 * LINEAR_TURN_WAVES) void linear_turn_kernel(
 #pragma unroll
         for (int j = 0; j < 4; ++j) out[64 * j] = *reinterpret_cast<const uint4*>(from + 16 * j);
     }
+}
+
+// gemm_sum_layer_kernel for dx (dx_groups workgroups to a token, `step` tokens side by side), and the sums of dbias in
+// workgroups of their own behind it.
+__global__ __launch_bounds__(256) void linear_sum_kernel(uint32_t n_parts, uint32_t n_tokens, uint32_t cols, LayerOut dst,
+                                                         uint32_t dx_groups, uint32_t step, const float* __restrict__ dbias_parts,
+                                                         uint32_t n_dbias_parts, uint32_t rows, float* __restrict__ dbias) {
+    if (blockIdx.x < dx_groups * step) gemm_sum_layer(blockIdx.x % dx_groups, blockIdx.x / dx_groups, step, n_parts, n_tokens, cols, dst);
+    else linear_dbias(blockIdx.x - dx_groups * step, dbias_parts, n_dbias_parts, rows, dbias);
 }
 
 }  // namespace bof4

@@ -185,11 +185,6 @@ int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t co
                               l.dbias_dev ? dbias_parts : nullptr, l.ld_dy, l.ld_pre, l.ld_mul, l.ld_dmul, l.act,
                               l.dy_type == BOF4_BF16, l.pre_type == BOF4_BF16, l.mul_type == BOF4_BF16, l.dmul_type == BOF4_BF16,
                               dy.wide8() && pre.wide8() && mul.wide8() && dmul.wide8()};
-    hipLaunchKernelGGL(linear_dz_kernel, dim3(row_chunks, P.ranges), dim3(256), 0, s, a, n_tokens, (uint32_t)rows, row_chunks,
-                       tok_tiles, P.tiles_per_range, xp);
-    if (l.dbias_dev)
-        hipLaunchKernelGGL(linear_dbias_kernel, dim3((uint32_t)((rows + 255) / 256)), dim3(256), 0, s, dbias_parts, P.ranges,
-                           (uint32_t)rows, l.dbias_dev);
     LayerOut out = {};
     out.y = l.dx_dev;
     out.ld_y = l.ld_dx;
@@ -202,21 +197,38 @@ int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t co
     // binary32 as well, so a sum over 11008 rows takes 22 of them.
     constexpr uint32_t FLUSH = 8;
     timing_begin(s);
+    // dz in the launch that turns the matrix or in one of its own, where it is not held to the few workgroups per compute unit
+    // that the other's LDS leaves (calls with all gradients, own launch / joint, us: 1024 x 1024 with 64 tokens 21.9 / 19.1, 4096 x
+    // 4096 with 333 / 1000 / 2000 39.9 / 38.5, 64.2 / 63.0, 100.2 / 101.2, 11008 x 4096 with 256 / 512 / 1000 / 2000 67.0 / 61.6, 89.5 /
+    // 87.4, 137.0 / 138.0, 230 / 244).
+    const bool dz_apart = (uint64_t)n_tokens * rows > (6ull << 20);
+    if (dz_apart)
+        hipLaunchKernelGGL(linear_dz_kernel, dim3(row_chunks, P.ranges), dim3(256), 0, s, a, n_tokens, (uint32_t)rows, row_chunks,
+                           tok_tiles, P.tiles_per_range, xp);
     for (uint32_t ct0 = 0; ct0 < col_tiles; ct0 += D.slab_tiles) {
         const uint32_t n_ct = col_tiles - ct0 < D.slab_tiles ? col_tiles - ct0 : D.slab_tiles;
         const uint64_t jobs = (uint64_t)((n_ct + 1) / 2) * row_chunks;
         const uint32_t groups = (n_ct + GEMM_WIDE_WAVES - 1) / GEMM_WIDE_WAVES;
+        const LinearDzCall dz = {a, ct0 == 0 && !dz_apart ? row_chunks * P.ranges : 0, n_tokens, (uint32_t)rows, tok_tiles, P.tiles_per_range, xp};
 #define BOF4_LAUNCH_TURN(OUT_)                                                                                          \
-    hipLaunchKernelGGL((linear_turn_kernel<OUT_>), dim3((uint32_t)((jobs + LINEAR_TURN_WAVES - 1) / LINEAR_TURN_WAVES)), \
+    hipLaunchKernelGGL((linear_turn_kernel<OUT_>),                                                                      \
+                       dim3(dz.dz_groups + (uint32_t)((jobs + LINEAR_TURN_WAVES - 1) / LINEAR_TURN_WAVES)),             \
                        dim3(64 * LINEAR_TURN_WAVES), 0, s, (const char*)packed_dev, ct0, n_ct, chunks, row_chunks, cb,  \
-                       offsets_dev, entries_dev, (uint32_t)n_outliers, T.lg, T.row_tiles, decoded);
+                       offsets_dev, entries_dev, (uint32_t)n_outliers, T.lg, T.row_tiles, decoded, dz);
         if (n_outliers > 0) { BOF4_LAUNCH_TURN(true) } else { BOF4_LAUNCH_TURN(false) }
 #undef BOF4_LAUNCH_TURN
         hipLaunchKernelGGL((gemm_decoded_kernel<false, LayerOut>), dim3(tok_groups * groups * D.split), dim3(64 * GEMM_WIDE_WAVES),
                            0, s, decoded, ct0 * GEMM_ROWS, n_ct, (uint32_t)cols, row_chunks, xp, tok_tiles, tok_groups, D.per_split,
                            FLUSH, n_tokens, D.split, out);
     }
-    if (D.split > 1) gemm_add_parts(D.split, n_tokens, cols, out, s);
+    const uint32_t dbias_groups = l.dbias_dev ? (uint32_t)((rows + 255) / 256) : 0;
+    if (D.split > 1) {
+        const uint32_t dx_groups = (uint32_t)((cols + 1023) / 1024), most = n_tokens < 65535 ? n_tokens : 65535;
+        hipLaunchKernelGGL(linear_sum_kernel, dim3(dx_groups * most + dbias_groups), dim3(256), 0, s, D.split, n_tokens, (uint32_t)cols,
+                           out, dx_groups, most, dbias_parts, P.ranges, (uint32_t)rows, l.dbias_dev);
+    } else if (l.dbias_dev) {
+        hipLaunchKernelGGL(linear_dbias_kernel, dim3(dbias_groups), dim3(256), 0, s, dbias_parts, P.ranges, (uint32_t)rows, l.dbias_dev);
+    }
     timing_end(s);
     HIP_TRY(hipGetLastError());
     return BOF4_OK;

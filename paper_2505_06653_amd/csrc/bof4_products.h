@@ -144,9 +144,10 @@ int gemm_run(const GemmCall& call, const GemmPlan& P, Out dst) {
     const uint32_t n_pad = (n_tokens + GEMM_TOKENS - 1) / GEMM_TOKENS * GEMM_TOKENS, tok_tiles = n_pad / GEMM_TOKENS;
     const uint4* xp = (const uint4*)((char*)ws_dev + L.xp);
     float* part = (float*)((char*)ws_dev + L.part);
-    if (!P.x_in_place) {
-        const uint64_t total = (uint64_t)tok_tiles * chunks * 256;
-        hipLaunchKernelGGL(gemm_pack_x_kernel, dim3((uint32_t)((total + 255) / 256)), dim3(256), 0, s,
+    const uint64_t x_words = (uint64_t)tok_tiles * chunks * 256;
+    const uint32_t pack_groups = (uint32_t)((x_words + 255) / 256);
+    if (!P.x_in_place && P.way != GEMM_DECODED) {
+        hipLaunchKernelGGL(gemm_pack_x_kernel, dim3(pack_groups), dim3(256), 0, s,
                            (const uint16_t*)x_dev, n_tokens, (uint32_t)cols, chunks, n_pad, (uint4*)xp);
     }
     timing_begin(s);
@@ -161,10 +162,11 @@ int gemm_run(const GemmCall& call, const GemmPlan& P, Out dst) {
             const uint32_t n_rt = T.row_tiles - rt0 < D.slab_tiles ? T.row_tiles - rt0 : D.slab_tiles;
             const uint64_t jobs = (uint64_t)n_rt * ((chunks + GEMM_DECODE_TILES - 1) / GEMM_DECODE_TILES);
             const uint32_t groups = (n_rt + GEMM_WIDE_WAVES - 1) / GEMM_WIDE_WAVES;
+            const uint32_t packing = rt0 == 0 ? pack_groups : 0, decoding = (uint32_t)((jobs + GEMM_DECODE_WAVES - 1) / GEMM_DECODE_WAVES);
 #define BOF4_LAUNCH_DECODE(OUT_)                                                                                       \
-    hipLaunchKernelGGL((gemm_decode_kernel<OUT_>), dim3((uint32_t)((jobs + GEMM_DECODE_WAVES - 1) / GEMM_DECODE_WAVES)), \
-                       dim3(64 * GEMM_DECODE_WAVES), 0, s, (const char*)packed_dev, rt0, n_rt, chunks, cb,             \
-                       offsets_dev, entries_dev, (uint32_t)n_outliers, T.lg, T.row_tiles, decoded);
+    hipLaunchKernelGGL((gemm_decode_kernel<OUT_>), dim3(packing + decoding), dim3(64 * GEMM_DECODE_WAVES), 0, s,       \
+                       (const char*)packed_dev, rt0, n_rt, chunks, cb, offsets_dev, entries_dev, (uint32_t)n_outliers, T.lg, \
+                       T.row_tiles, decoded, packing, (const uint16_t*)x_dev, n_tokens, (uint32_t)cols, n_pad, (uint4*)xp);
 #define BOF4_LAUNCH_DECODED(CARRY_)                                                                                    \
     hipLaunchKernelGGL((gemm_decoded_kernel<CARRY_, Out>), dim3(tok_groups * groups * D.split), dim3(64 * GEMM_WIDE_WAVES), \
                        0, s, decoded, rt0 * GEMM_ROWS, n_rt, (uint32_t)rows, chunks, xp, tok_tiles, tok_groups,        \
