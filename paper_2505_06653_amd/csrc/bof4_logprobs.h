@@ -167,7 +167,7 @@ __device__ __forceinline__ uint64_t readlane64(uint64_t v, uint32_t lane) {
 //   With few rows a row is cut into n_splits parts, one per workgroup, whose records logprobs_join_kernel joins.
 constexpr uint32_t LOGPROBS_WORDS = 4, LOGPROBS_JOIN_WAVES = 16; // 16-byte words per lane and tile; waves per row that joins
 constexpr uint32_t LOGPROBS_TILE = 64 * LOGPROBS_WORDS;                // words
-constexpr uint32_t LOGPROBS_MAX_SPLITS = 64, LOGPROBS_TARGET_WGS = 1024;
+constexpr uint32_t LOGPROBS_MAX_SPLITS = 64;
 constexpr uint32_t logprobs_word_elements(bool bf16) { return bf16 ? 8 : 4; }
 
 struct LogprobsPart {  // what a part of a row leaves: its sums, then `top` keys

@@ -72,7 +72,7 @@ def make(n, vocab, dtype, seed, spread=2.5):
 
 
 SHAPES = [(1, 1), (2, 2), (1, 5), (3, 63), (3, 64), (5, 65), (2, 1000), (300, 2049), (7, 50257), (3, 128000), (1, 300001),
-          (1000, 1023), (2, 4096), (2, 4097), (515, 8193)]
+          (1000, 1023), (2, 4096), (2, 4097), (515, 8193), (1030, 2047), (1025, 100003)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
@@ -266,7 +266,7 @@ def test_gradient_in_place_into_strided_rows_and_nothing_else(dtype):
     assert torch.equal(view, want) and (wide[:, :3] == 7).all() and (wide[:, 3 + vocab:] == 7).all()
 
 
-@pytest.mark.parametrize("n,vocab", [(2, 100003), (700, 3001)])
+@pytest.mark.parametrize("n,vocab", [(2, 100003), (700, 3001), (1100, 2001)])
 def test_equal_bits_on_every_call_other_streams_and_captured(n, vocab):
     x, t = make(n, vocab, torch.float32, 9)
     g = torch.ones(n, device=DEV)
