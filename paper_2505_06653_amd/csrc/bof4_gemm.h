@@ -872,15 +872,19 @@ __global__ __launch_bounds__(64 * GEMM_DECODE_WAVES) void gemm_decode_kernel(
 // the same order: where the columns are split alike, the results are gemm_wide_kernel's bit for bit.
 //   Operands go from memory to LDS without passing through registers (the tiles lie in memory as they lie in LDS: a wave's
 // request is 1024 bytes on either side), one row tile and a share of x per wave and chunk.  A step's one barrier stands in
-// front of its last quarter: by then every wave has its last words of the step's buffer in registers, so chunk s + 3 may come
-// into it, and has waited for its own share of chunk s + 1 (six requests; the six of chunk s + 2 stay on their way), so the
-// last quarter can already ask for the next step's first words.  A request has two steps' time.
-//   What bounds it: the matrix cores' rate at the clock that the card holds meanwhile (1.8 GHz); 1.1 to 1.2 PFLOP/s, where a large
-// product of the library reaches 1.17 to 1.22.  One product per two LDS reads in the order of issue: 2 to 3 % faster than four
-// products after four reads; the waves' priority raised for the products 4 to 8 % slower; the tiles' sums carried in turns no
-// difference.  Against bringing the operands in through registers, gradient calls whole, 11008 x 4096 with 2000 tokens 226 ->
-// 213 us, 4096 x 11008 248 -> 232, 22016 x 4096 with 4096 828 -> 782; with the barrier at the step's end, where a request has one
-// step, 219 -> 206 on one card and 800 -> 885 on the largest; 128 x 128 tiles in four waves, two workgroups a compute unit, 248.
+// front of its third quarter: by then every wave has its last words of the step's buffer in registers (operands are read two
+// quarters ahead), so chunk s + 3 may come into it, and has waited for its own share of chunk s + 1 (six requests; the six of
+// chunk s + 2 stay on their way), so what is left of the step can already ask for the next step's first words.  A request has
+// two steps' time.
+//   What bounds it (4096 columns of the result x 2000 tokens, chains of 11008): the matrix cores are busy 56 % of the time at the 1.91
+// GHz that the card holds meanwhile, the vector units 20 %; 1.1 PFLOP/s, where a large product of the library reaches 1.17 to
+// 1.22.  The rest is what eight waves wait for each other at the barriers: neither LDS latency (operands one quarter ahead: 1 %
+// slower) nor the way from the caches (a fifth less traffic by the bands below: no difference there).  One product per two LDS
+// reads in the order of issue: 2 to 3 % faster than four products after four reads; the waves' priority raised for the
+// products 4 to 8 % slower; the tiles' sums carried in turns no difference.
+//   Against bringing the operands in through registers, gradient calls whole, 11008 x 4096 with 2000 tokens 226 -> 213 us, 4096 x
+// 11008 248 -> 232, 22016 x 4096 with 4096 828 -> 782; with the barrier at the step's end, where a request has one step, 219 ->
+// 206 on one card and 800 -> 885 on the largest; 128 x 128 tiles in four waves, two workgroups a compute unit, 248.
 //   2000 tokens with a list, gemm_wide_kernel -> decoding and this (through registers): 4096 x 4096 127 -> 102 us, 12288 x 4096
 // 353 -> 252, 22016 x 4096 649 -> 482, 8192 x 28672 1305 -> 1042.
 constexpr int GEMM_WAIT_ALL_LDS = 0x0f70;        // s_waitcnt: no request on its way into LDS
@@ -905,14 +909,18 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
     __shared__ __attribute__((aligned(16))) Shared sh;
     const uint32_t tid = threadIdx.x, lane = tid & 63;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // (as in gemm_wide_kernel: each die takes a contiguous run of tiles, token groups fastest)
+    // As in gemm_wide_kernel each die takes a contiguous run of tiles; it goes through bands of four row groups, token group by
+    // token group, so that its 32 compute units share four row groups and eight token groups at a time, the least to read
+    // for 32 tiles of 256 x 128 (token groups fastest: 22016 x 4096 with 4096 tokens 848 us instead of 780).
     uint32_t id = blockIdx.x;
     {
         const uint32_t total = gridDim.x, q = total / 8, rem = total % 8, die = id % 8;
         id = die * q + min(die, rem) + id / 8;
     }
     const uint32_t row_groups = (n_rt + GEMM_WIDE_WAVES - 1) / GEMM_WIDE_WAVES;
-    const uint32_t tg = id % tok_groups, rg = (id / tok_groups) % row_groups, part = id / (tok_groups * row_groups);
+    const uint32_t part = id / (tok_groups * row_groups), place = id - part * tok_groups * row_groups;
+    const uint32_t band = place / (4 * tok_groups), in_band = place - band * 4 * tok_groups, height = min(4u, row_groups - 4 * band);
+    const uint32_t tg = in_band / height, rg = 4 * band + in_band % height;
     const uint32_t ch0 = part * per_split, ch1 = min(n_chunks, ch0 + per_split), n_steps = ch1 - ch0;
     // a row tile or token tile past the last is read from the last one and not stored
     const uint4* my_a = decoded + (uint64_t)min(rg * GEMM_WIDE_WAVES + wave, n_rt - 1) * n_chunks * GEMM_TILE_WORDS + lane;
@@ -947,19 +955,19 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
         return o;
     };
     uint32_t until_flush = flush;
-    // Before step s: chunk s is in buffer s % 3, chunks s + 1 and s + 2 are on their way into the next two; `op` are the operands
-    // of the step's first quarter.
-    Operands op;
+    // Before step s: chunk s is in buffer s % 3, chunks s + 1 and s + 2 are on their way into the next two; `op` and `op1` are the
+    // operands of the step's first two quarters.
+    Operands op, op1;
     auto step = [&](uint32_t s, const uint32_t buf) __attribute__((always_inline)) {
         const uint32_t buf1 = buf == 2u ? 0u : buf + 1u;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if (j == 3) {
+            if (j == 2) {
                 __builtin_amdgcn_s_waitcnt(GEMM_WAIT_BUT_6_AND_READS);
                 gemm_bare_barrier();
                 bring(s + 3, buf);
             }
-            const Operands next = read_operands(j < 3 ? buf : buf1, (j + 1) & 3);
+            const Operands next = read_operands(j < 2 ? buf : buf1, (j + 2) & 3);
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -971,7 +979,8 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
             __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
             __builtin_amdgcn_sched_barrier(0);
-            op = next;
+            op = op1;
+            op1 = next;
         }
         if (--until_flush == 0u) {
             until_flush = flush;
@@ -996,6 +1005,7 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
     __builtin_amdgcn_s_waitcnt(GEMM_WAIT_BUT_12);
     gemm_bare_barrier();
     op = read_operands(0, 0);
+    op1 = read_operands(0, 1);
     uint32_t s = 0;  // (three steps to a round, so that the buffers' places do not move)
     for (uint32_t rounds = n_steps / 3; rounds > 0; --rounds, s += 3) {
         step(s, 0);
