@@ -687,6 +687,25 @@ def _layer_input(x, cols, gpu):
     return x2
 
 
+def _table(table, rows, cols, n_outliers, gpu):
+    """The address of an outlier table for that matrix and list, or None without a list."""
+    k = int(n_outliers)
+    if k == 0:
+        return None, 0
+    if table is None:
+        raise ValueError("outliers need their table (bof4_gemv_outlier_table, bof4_gemm_outlier_table)")
+    # (bof4_gemv_outlier_table_bytes)
+    if table.get_device() != gpu or table.numel() < (((rows * -(-cols // 2048) + 1) * 4 + 7) & ~7) + 8 * k:
+        raise ValueError("the outlier table must be on the current GPU and have bof4_gemv_outlier_table_bytes(rows, cols, n_outliers) bytes")
+    return table.data_ptr(), k
+
+
+def _packed(packed, rows, cols, gpu):
+    if packed.get_device() != gpu or packed.numel() < bof4_gemm_packed_bytes(rows, cols):
+        raise ValueError("the packed matrix must be on the current GPU and not too small for rows x cols (bof4_gemm_pack)")
+    return packed.data_ptr()
+
+
 def _layer(n_tokens, rows, bias, act, mul, residual, pre, out, gpu):
     shape = (n_tokens, rows)
     bias_at = mul_at = residual_at = pre_at = bias_type = mul_type = residual_type = pre_type = ld_mul = ld_residual = ld_pre = 0
@@ -712,14 +731,15 @@ def bof4_gemv_linear(codes, scales, rows, cols, block, cb, x, table=None, n_outl
     cb, cbp = _cb(cb)
     gpu = torch.cuda.current_device()
     x2 = _layer_input(x, cols, gpu)
-    n_tokens, k = x2.shape[0], int(n_outliers)
-    if k and table is None:
-        raise ValueError("outliers need their table (bof4_gemv_outlier_table)")
+    n_tokens = x2.shape[0]
+    table_at, k = _table(table, rows, cols, n_outliers, gpu)
+    if codes.get_device() != gpu or scales.get_device() != gpu or 2 * codes.numel() < rows * cols or scales.numel() * block < rows * cols:
+        raise ValueError("codes and scales must be on the current GPU and have those of rows x cols weights")
     if out is None:
         out = torch.empty((n_tokens, rows), dtype=out_dtype, device=x.device)
     layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out, gpu)
-    _check(lib().bof4_gemv_linear(codes.data_ptr(), scales.data_ptr(), rows, cols, block, cbp, table.data_ptr() if k else None, k,
-                                  x2.data_ptr(), n_tokens, layer, _stream(stream)))
+    _check(lib().bof4_gemv_linear(codes.data_ptr(), scales.data_ptr(), rows, cols, block, cbp, table_at, k, x2.data_ptr(),
+                                  n_tokens, layer, _stream(stream)))
     return out
 
 
@@ -734,17 +754,15 @@ def bof4_gemm_linear(packed, rows, cols, cb, x, table=None, n_outliers=0, bias=N
     cb, cbp = _cb(cb)
     gpu = torch.cuda.current_device()
     x2 = _layer_input(x, cols, gpu)
-    if packed.numel() < bof4_gemm_packed_bytes(rows, cols):
-        raise ValueError("packed matrix too small for rows x cols (bof4_gemm_pack)")
-    n_tokens, k = x2.shape[0], int(n_outliers)
-    if k and table is None:
-        raise ValueError("outliers need their table (bof4_gemm_outlier_table)")
+    packed_at = _packed(packed, rows, cols, gpu)
+    n_tokens = x2.shape[0]
+    table_at, k = _table(table, rows, cols, n_outliers, gpu)
     if out is None:
         out = torch.empty((n_tokens, rows), dtype=out_dtype, device=x.device)
     layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out, gpu)
     ws = _scratch(ws, 0 if ws is not None else bof4_gemm_linear_workspace_bytes(rows, cols, n_tokens), x.device, stream)
-    _check(lib().bof4_gemm_linear(packed.data_ptr(), rows, cols, cbp, table.data_ptr() if k else None, k, x2.data_ptr(),
-                                  n_tokens, layer, ws.data_ptr(), ws.numel(), _stream(stream)))
+    _check(lib().bof4_gemm_linear(packed_at, rows, cols, cbp, table_at, k, x2.data_ptr(), n_tokens, layer, ws.data_ptr(),
+                                  ws.numel(), _stream(stream)))
     return out
 
 
@@ -760,14 +778,12 @@ def bof4_gemm_linear_backward(packed, rows, cols, cb, dy, table=None, n_outliers
     cb, cbp = _cb(cb)
     if dy.dim() != 2 or dy.shape[1] != rows:
         raise ValueError("dy must be [n_tokens, rows]")
-    if packed.numel() < bof4_gemm_packed_bytes(rows, cols):
-        raise ValueError("packed matrix too small for rows x cols (bof4_gemm_pack)")
-    n_tokens, k = int(dy.shape[0]), int(n_outliers)
-    if k and table is None:
-        raise ValueError("outliers need their table (bof4_gemm_outlier_table)")
+    gpu, n_tokens = torch.cuda.current_device(), dy.shape[0]
+    packed_at = _packed(packed, rows, cols, gpu)
+    table_at, k = _table(table, rows, cols, n_outliers, gpu)
     if out is None:
         out = torch.empty((n_tokens, cols), dtype=out_dtype, device=dy.device)
-    gpu, shape = torch.cuda.current_device(), (n_tokens, rows)
+    shape = (n_tokens, rows)
     pre_at = mul_at = dmul_at = dbias_at = pre_type = mul_type = dmul_type = ld_pre = ld_mul = ld_dmul = 0
     dy_at, dx_at = _tensor(dy, "dy", _TYPES, shape, gpu), _tensor(out, "out", _TYPES, (n_tokens, cols), gpu)
     if pre is not None:
@@ -781,8 +797,8 @@ def bof4_gemm_linear_backward(packed, rows, cols, cb, dy, table=None, n_outliers
     g = LAYER_GRADIENT.pack(_activation(act), _TYPES[dy.dtype], pre_type, mul_type, dmul_type, _TYPES[out.dtype], dy_at, pre_at,
                             mul_at, dmul_at, dbias_at, dx_at, _row_stride(dy), ld_pre, ld_mul, ld_dmul, _row_stride(out))
     ws = _scratch(ws, 0 if ws is not None else bof4_gemm_linear_backward_workspace_bytes(rows, cols, n_tokens), dy.device, stream)
-    _check(lib().bof4_gemm_linear_backward(packed.data_ptr(), rows, cols, cbp, table.data_ptr() if k else None, k, n_tokens, g,
-                                           ws.data_ptr(), ws.numel(), _stream(stream)))
+    _check(lib().bof4_gemm_linear_backward(packed_at, rows, cols, cbp, table_at, k, n_tokens, g, ws.data_ptr(), ws.numel(),
+                                           _stream(stream)))
     return out
 
 

@@ -251,7 +251,8 @@ def test_activations_far_out():
 
 
 # ------------------------------------------------------------------------------------------------ gradients
-GRAD = [(1, 32, 1, 0.0), (3, 64, 5, 0.1), (65, 96, 40, 0.05), (100, 2080, 33, 0.02), (1001, 1504, 300, 0.0), (33, 32768, 40, 0.001),
+# dz with the turned matrix and apart from it, one slab and two, rows split and not
+GRAD = [(1, 32, 1, 0.0), (70001, 160, 100, 0.01), (3, 64, 5, 0.1), (65, 96, 40, 0.05), (100, 2080, 33, 0.02), (1001, 1504, 300, 0.0), (33, 32768, 40, 0.001),
         (16390, 128, 70, 0.01), (4111, 4128, 333, 0.006), (2050, 2080, 2001, 0.003), (70001, 160, 9, 0.01), (9000, 16384, 130, 0.002),
         (64, 224, 130, 0.9)]
 
@@ -417,6 +418,30 @@ def test_equal_bits_streams_workspaces_and_captured(rows, cols, n_tokens):
             assert torch.equal(a, b)
 
 
+def test_two_calls_side_by_side_on_two_streams():
+    """Each with a workspace of its own, forward and back, while the other runs: what each gives alone."""
+    shapes = [(4111, 4128, 300), (1001, 2080, 600)]
+    ms = [Matrix(r, c, 0.01) for r, c, _ in shapes]
+    xs = [randn((n, c), 1) for _, c, n in shapes]
+    dys = [randn((n, r), 2) for r, _, n in shapes]
+
+    def run(i, stream=None):
+        y = ms[i].linear("gemm", xs[i], act="relu", stream=stream)
+        v = ms[i].linear("gemv", xs[i][:3].contiguous(), act="relu", stream=stream)
+        return y, v, ms[i].backward(dys[i], stream=stream)
+
+    want = [run(i) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[run(i, streams[i]) for i in range(2)] for _ in range(4)]
+    torch.cuda.synchronize()
+    for round_ in got:
+        for a, b in zip(round_, want):
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
 def test_least_workspace_takes_another_way_and_less_is_refused():
     rows, cols, n_tokens = 2050, 2080, 2001
     m = Matrix(rows, cols, 0.003)
@@ -448,6 +473,18 @@ def test_refusals():
         out2, r2 = _two_types((3, 64))
         with pytest.raises(binding.Bof4Error):  # over the residual with another type
             m.linear(way, x, residual=r2, out=out2)
+    w = m.codes, m.scales, 64, 96, 32, m.cb, x
+    p = m.packed, 64, 96, m.cb
+    for call in (lambda: binding.bof4_gemv_linear(*w, None, m.k), lambda: binding.bof4_gemv_linear(*w, m.gemv_table[:-8], m.k),
+                 lambda: binding.bof4_gemv_linear(*w, m.gemv_table.cpu(), m.k), lambda: binding.bof4_gemv_linear(m.codes[1:], *w[1:]),
+                 lambda: binding.bof4_gemv_linear(m.codes, m.scales[1:], *w[2:]), lambda: binding.bof4_gemv_linear(m.codes.cpu(), *w[1:]),
+                 lambda: binding.bof4_gemm_linear(*p, x, None, m.k), lambda: binding.bof4_gemm_linear(*p, x, m.gemm_table[:-8], m.k),
+                 lambda: binding.bof4_gemm_linear(m.packed[1:], *p[1:], x), lambda: binding.bof4_gemm_linear(m.packed.cpu(), *p[1:], x),
+                 lambda: binding.bof4_gemm_linear(*p, x.cpu()), lambda: binding.bof4_gemm_linear(*p, x, ws=torch.empty(1 << 24)),
+                 lambda: binding.bof4_gemm_linear_backward(*p, r, m.gemm_table[:-8], m.k),
+                 lambda: binding.bof4_gemm_linear_backward(m.packed[1:], *p[1:], r), lambda: binding.bof4_gemm_linear_backward(*p, r.cpu())):
+        with pytest.raises(ValueError):
+            call()
     for bad in (dict(act="silu"), dict(dmul=r.clone()), dict(dmul=r.clone(), mul=r), dict(dbias=r[0]), dict(dbias=torch.empty(63, device=DEV))):
         with pytest.raises((ValueError, binding.Bof4Error)):
             m.backward(r, **bad)
