@@ -480,7 +480,8 @@ int bof4_token_logprobs_backward(const void* logits_dev, uint32_t logits_type, u
                                  const float* d_logprob_dev, const float* entropy_dev, const float* d_entropy_dev,
                                  void* d_logits_dev, uint32_t d_logits_type, uint64_t ld_d_logits, void* stream);
 
-/* Measurement aid: the next bof4_quantize / bof4_dequantize / bof4_lloyd_step / bof4_quant_error / bof4_gemv / bof4_gemm call made by this thread records
+/* Measurement aid: the next bof4_quantize / bof4_dequantize / bof4_lloyd_step / bof4_quant_error / bof4_gemv / bof4_gemm call, or call of
+ * a linear layer or of token log probabilities (or of a gradient of theirs), made by this thread records
  * the caller-owned hipEvent_t `start_event` immediately before and `stop_event` immediately after its main kernel
  * (the one that streams over the weights), on the call's stream; helper kernels and host synchronisation lie
  * outside the pair.  The request is consumed by that call.  Pass NULLs to cancel. */

@@ -876,7 +876,7 @@ __global__ __launch_bounds__(64 * GEMM_DECODE_WAVES) void gemm_decode_kernel(
 // quarters ahead), so chunk s + 3 may come into it, and has waited for its own share of chunk s + 1 (six requests; the six of
 // chunk s + 2 stay on their way), so what is left of the step can already ask for the next step's first words.  A request has
 // two steps' time.
-//   What bounds it (4096 columns of the result x 2000 tokens, chains of 11008): the matrix cores are busy 56 % of the time at the 1.91
+//   What bounds it (4096 columns of the result x 2000 tokens, chains of 11008): the matrix cores are busy 55 % of the time at the 1.96
 // GHz that the card holds meanwhile, the vector units 20 %; 1.1 PFLOP/s, where a large product of the library reaches 1.17 to
 // 1.22.  The rest is what eight waves wait for each other at the barriers: neither LDS latency (operands one quarter ahead: 1 %
 // slower) nor the way from the caches (a fifth less traffic by the bands below: no difference there).  One product per two LDS
