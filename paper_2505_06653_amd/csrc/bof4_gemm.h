@@ -884,7 +884,8 @@ __global__ __launch_bounds__(64 * GEMM_DECODE_WAVES) void gemm_decode_kernel(
 // products 4 to 8 % slower; the tiles' sums carried in turns no difference.
 //   Against bringing the operands in through registers, gradient calls whole, 11008 x 4096 with 2000 tokens 226 -> 213 us, 4096 x
 // 11008 248 -> 232, 22016 x 4096 with 4096 828 -> 782; with the barrier at the step's end, where a request has one step, 219 ->
-// 206 on one card and 800 -> 885 on the largest; 128 x 128 tiles in four waves, two workgroups a compute unit, 248.
+// 206 on one card and 800 -> 885 on the largest; 128 x 128 tiles in four waves, two workgroups a compute unit, 248; the waves in
+// two groups, one reading a whole chunk's operands while the other multiplies, 11008 x 4096 227 -> 249, 22016 x 4096 780 -> 865.
 //   2000 tokens with a list, gemm_wide_kernel -> decoding and this (through registers): 4096 x 4096 127 -> 102 us, 12288 x 4096
 // 353 -> 252, 22016 x 4096 649 -> 482, 8192 x 28672 1305 -> 1042.
 constexpr int GEMM_WAIT_ALL_LDS = 0x0f70;        // s_waitcnt: no request on its way into LDS
