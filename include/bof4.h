@@ -388,8 +388,7 @@ size_t bof4_gemm_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t n_tokens
 #define BOF4_ACT_GELU_TANH 3u /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
 #define BOF4_ACT_SILU 4u      /* z / (1 + exp(-z)) */
 /* What belongs to a layer besides the matrix (host struct, read during the call).  Types are BOF4_F32 or BOF4_BF16; ld_* are
- * elements from one token to the next (>= rows); every pointer has its element's alignment (four elements' alignment of all
- * pointers and row strides saves time). */
+ * elements from one token to the next (>= rows); every pointer has its element's alignment. */
 typedef struct {
     uint32_t act;                                               /* BOF4_ACT_*                                        */
     uint32_t bias_type, mul_type, residual_type, y_type, pre_type;

@@ -213,6 +213,11 @@ __device__ __forceinline__ void wave_lds_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// Several elements in one access wherever they lie (global memory takes any alignment; only lines crossed cost extra).
+typedef uint32_t u32_any __attribute__((aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
 // Two numbers rounded to bfloat16 (to nearest even), the first in the low half (one instruction).
 typedef __bf16 gemm_bf16x2 __attribute__((ext_vector_type(2)));
 typedef float gemm_f32x2 __attribute__((ext_vector_type(2)));

@@ -1065,12 +1065,11 @@ __device__ __forceinline__ void gemm_sum_layer(uint32_t group, uint32_t first, u
     const uint64_t count = (uint64_t)n_tokens * rows;
     for (uint32_t token = first; token < n_tokens; token += step) {
         const float* p = dst.parts + (uint64_t)token * rows + row;
-        const bool whole = row + 4 <= rows && (rows & 3u) == 0u;
         double s[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 4
         for (uint32_t k = 0; k < n_parts; ++k) {
             float v[4];
-            load_row<4>(p + k * count, 0, false, whole, rows - row, v);
+            load_row<4>(p + k * count, 0, false, rows - row, v);
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[i] += v[i];
         }

@@ -5,7 +5,7 @@
 // dx contracts over the rows of W^, so the matrix cores want it turned.  A call works in two steps, as the product for many
 // tokens does whose matrix is decoded first: linear_turn_kernel decodes the packed matrix into the operands of W^^T, in
 // slabs that stay in the cache behind the L2s, and gemm_decoded_kernel multiplies them with dz.  dz is rounded to bfloat16
-// once, which is what the matrix cores take: each term is off by 2^-9 of itself at most, as far as dx's own rounding to
+// once, which is what the matrix cores take: each term is off by 2^-8 of itself at most, as far as dx's own rounding to
 // bfloat16 (without activation and factor dz is dy, and nothing is rounded).  linear_dz makes it from dy in the
 // order of the operands, and dmul and dbias on the way.
 #pragma once
@@ -25,7 +25,6 @@ struct LinearGradArgs {
     uint64_t ld_dy, ld_pre, ld_mul, ld_dmul;
     uint32_t act;
     bool dy_bf16, pre_bf16, mul_bf16, dmul_bf16;
-    bool wide;  // eight neighbouring elements of every tensor begin on 16 bytes
 };
 
 // dz in the products' order (gemm_pack_x_kernel's, rows in the place of columns): a workgroup takes a chunk of 64 rows and
@@ -46,11 +45,10 @@ __device__ __forceinline__ void linear_dz(uint32_t chunk, uint32_t range, Linear
         uint32_t w[4] = {0u, 0u, 0u, 0u};
         if (t < n_tokens && row < rows) {
             const uint32_t n = rows - row;
-            const bool whole = a.wide && n >= 8;
             float dy[8], z[8] = {}, f[8], value, slope;
-            load_row<8>(a.dy, t * a.ld_dy + row, a.dy_bf16, whole, n, dy);
-            if (a.pre) load_row<8>(a.pre, t * a.ld_pre + row, a.pre_bf16, whole, n, z);
-            if (a.mul) load_row<8>(a.mul, t * a.ld_mul + row, a.mul_bf16, whole, n, f);
+            load_row<8>(a.dy, t * a.ld_dy + row, a.dy_bf16, n, dy);
+            if (a.pre) load_row<8>(a.pre, t * a.ld_pre + row, a.pre_bf16, n, z);
+            if (a.mul) load_row<8>(a.mul, t * a.ld_mul + row, a.mul_bf16, n, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 activation_slope(a.act, z[i], value, slope);
@@ -60,7 +58,7 @@ __device__ __forceinline__ void linear_dz(uint32_t chunk, uint32_t range, Linear
                 if ((uint32_t)i >= n) dy[i] = 0.0f;
                 bias[i] += dy[i];
             }
-            if (a.dmul) store_row<8>(a.dmul, t * a.ld_dmul + row, a.dmul_bf16, whole, n, z);
+            if (a.dmul) store_row<8>(a.dmul, t * a.ld_dmul + row, a.dmul_bf16, n, z);
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = gemm_pack_bf16(dy[2 * i], dy[2 * i + 1]);
         }

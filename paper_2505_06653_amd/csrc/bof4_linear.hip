@@ -25,8 +25,6 @@ struct Rows {
     uint32_t type;
     uint64_t ld;
     bool ok(uint64_t rows) const { return !p || (valid_type(type) && aligned(p, type_bytes(type)) && ld >= rows); }
-    bool wide() const { return !p || (aligned(p, 4 * type_bytes(type)) && ld % 4 == 0); }    // four elements in one access
-    bool wide8() const { return !p || (aligned(p, 16) && ld % (16 / type_bytes(type)) == 0); }  // eight, 16 bytes each
     // the other tensor of the same elements, or another place altogether
     bool same_or_apart(const Rows& o) const { return !p || p != o.p || (type == o.type && ld == o.ld); }
 };
@@ -48,9 +46,7 @@ int layer_out(const bof4_layer* layer, uint64_t rows, const void* x_dev, LayerOu
         return fail(BOF4_ERR_ARG, "linear layer: y and pre need memory of their own");
     *out = LayerOut{l.bias_dev, l.mul_dev, l.residual_dev, l.y_dev, l.pre_dev, l.ld_mul, l.ld_residual, l.ld_y, l.ld_pre, l.act,
                     l.bias_type == BOF4_BF16, l.mul_type == BOF4_BF16, l.residual_type == BOF4_BF16, l.y_type == BOF4_BF16,
-                    l.pre_type == BOF4_BF16,
-                    (!bias.p || aligned(bias.p, 4 * type_bytes(bias.type))) && mul.wide() && residual.wide() && y.wide() && pre.wide(),
-                    0, nullptr};
+                    l.pre_type == BOF4_BF16, 0, nullptr};
     return BOF4_OK;
 }
 
@@ -183,13 +179,11 @@ int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t co
     const uint32_t tok_groups = (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES;
     const LinearGradArgs a = {l.dy_dev, l.act != ACT_NONE || l.dmul_dev ? l.pre_dev : nullptr, l.mul_dev, l.dmul_dev,
                               l.dbias_dev ? dbias_parts : nullptr, l.ld_dy, l.ld_pre, l.ld_mul, l.ld_dmul, l.act,
-                              l.dy_type == BOF4_BF16, l.pre_type == BOF4_BF16, l.mul_type == BOF4_BF16, l.dmul_type == BOF4_BF16,
-                              dy.wide8() && pre.wide8() && mul.wide8() && dmul.wide8()};
+                              l.dy_type == BOF4_BF16, l.pre_type == BOF4_BF16, l.mul_type == BOF4_BF16, l.dmul_type == BOF4_BF16};
     LayerOut out = {};
     out.y = l.dx_dev;
     out.ld_y = l.ld_dx;
     out.y_bf16 = l.dx_type == BOF4_BF16;
-    out.wide = dx.wide();
     out.parts = (float*)(ws + P.parts);
     const GemmDecodedPlan& D = P.turned;
     const uint32_t col_tiles = (uint32_t)(cols / GEMM_ROWS);

@@ -445,8 +445,7 @@ __global__ __launch_bounds__(64 * LOGPROBS_JOIN_WAVES) void logprobs_join_kernel
 }
 
 // d x_j = g (delta_jt - p_j) - h p_j (log p_j + H), g and h the gradients of the row's log probability and entropy: read
-// once, written once.  A workgroup takes a stretch of a row, in 16-byte words of the logits as they lie in memory; their
-// gradients leave in wide stores where the output's rows are aligned alike.
+// once, written once.  A workgroup takes a stretch of a row, in 16-byte words of the logits as they lie in memory.
 struct LogprobsGradArgs {
     const void* logits;
     void* out;
@@ -470,7 +469,6 @@ __global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobsGradArgs a, 
     const uint32_t end = off + a.vocab, n_words = (end + PER_WORD - 1) / PER_WORD;
     const uint32_t w0 = stretch * 256 * WORDS + threadIdx.x;
     char* out = static_cast<char*>(a.out) + (uint64_t)row * a.ld_out * OUT_SIZE - (uint64_t)off * OUT_SIZE;
-    const bool wide = (reinterpret_cast<uintptr_t>(out) & (PER_WORD * OUT_SIZE < 16 ? PER_WORD * OUT_SIZE - 1 : 15u)) == 0u;
     const float m = a.stats[2 * (uint64_t)row], log_s = a.stats[2 * (uint64_t)row + 1];
     const int64_t t = a.target ? a.target[row] : -1;
     const bool asked = t >= 0 && t < (int64_t)a.vocab;
@@ -521,26 +519,18 @@ __global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobsGradArgs a, 
             for (uint32_t i = 0; i < PER_WORD; ++i)
                 if (first + i == target && !nothing) d[i] += g;
         }
-        if (!wide) {
-#pragma unroll
-            for (uint32_t i = 0; i < PER_WORD; ++i) {
-                if constexpr (OUT_BF16) reinterpret_cast<uint16_t*>(out)[first + i] = (uint16_t)f32_to_bf16_rne(d[i]);
-                else reinterpret_cast<float*>(out)[first + i] = d[i];
-            }
-            continue;
-        }
         char* to = out + (uint64_t)first * OUT_SIZE;
         if constexpr (OUT_BF16) {
             uint32_t o[PER_WORD / 2];
 #pragma unroll
             for (uint32_t i = 0; i < PER_WORD / 2; ++i) o[i] = gemm_pack_bf16(d[2 * i], d[2 * i + 1]);
-            if constexpr (PER_WORD == 8) store_stream(reinterpret_cast<uint4*>(to), make_uint4(o[0], o[1], o[2], o[3]));
-            else *reinterpret_cast<uint2*>(to) = make_uint2(o[0], o[1]);
+            if constexpr (PER_WORD == 8) __builtin_nontemporal_store(u32x4_any{o[0], o[1], o[2], o[3]}, reinterpret_cast<u32x4_any*>(to));
+            else *reinterpret_cast<u32x2_any*>(to) = u32x2_any{o[0], o[1]};
         } else {
 #pragma unroll
             for (uint32_t i = 0; i < PER_WORD; i += 4)
-                store_stream(reinterpret_cast<uint4*>(to) + i / 4, make_uint4(__float_as_uint(d[i]), __float_as_uint(d[i + 1]),
-                                                                            __float_as_uint(d[i + 2]), __float_as_uint(d[i + 3])));
+                __builtin_nontemporal_store(u32x4_any{__float_as_uint(d[i]), __float_as_uint(d[i + 1]), __float_as_uint(d[i + 2]),
+                                                      __float_as_uint(d[i + 3])}, reinterpret_cast<u32x4_any*>(to) + i / 4);
         }
     }
 }
