@@ -485,20 +485,20 @@ __global__ __launch_bounds__(64 * GEMM_MAX_WAVES, X_IN_PLACE ? 4 : 2) void gemm_
     }
 }
 
-// A layer's result of the 2 x 2 tiles of a wave of the 256 x 128 tile: each is turned in LDS, so that a lane holds four
+// A layer's result of a wave's tiles of the kernels for many tokens: each is turned in LDS, so that a lane holds four
 // neighbouring rows of one token and eight lanes write 64 bytes (or 128) of it; one copy of the layer's code in a loop,
 // where 64 sums in registers would need as many.
 constexpr uint32_t GEMM_STAGE_LD = 40;  // floats from one token to the next: the two halves of a wave meet in no bank
-template <class Out>
-__device__ __forceinline__ void gemm_store_tiles(const Out& dst, void* lds, uint32_t wave, uint32_t lane, gemm_f32x16 (&sum)[2][2],
-                                                 gemm_f32x16 (&acc)[2][2], uint32_t row0, uint32_t rows, uint32_t token0,
+template <class Out, int RW, int TW>
+__device__ __forceinline__ void gemm_store_tiles(const Out& dst, void* lds, uint32_t wave, uint32_t lane, gemm_f32x16 (&sum)[RW][TW],
+                                                 gemm_f32x16 (&acc)[RW][TW], uint32_t row0, uint32_t rows, uint32_t token0,
                                                  uint32_t n_tokens) {
     float* stage = reinterpret_cast<float*>(lds) + wave * (GEMM_TOKENS * GEMM_STAGE_LD);
     __syncthreads();  // the operands that stood here have been read
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
+    for (int r = 0; r < RW; ++r) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < TW; ++t) {
             wave_lds_fence();
 #pragma unroll
             for (int i = 0; i < 16; ++i)
@@ -750,7 +750,7 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_wide_kernel(
 
     if constexpr (Out::LAYER) {
         if (n_parts == 1) {
-            gemm_store_tiles(dst, &sh.a[0][0][0], wave, lane, sum, acc, (rg * GEMM_WIDE_WAVES + wr) * GEMM_ROWS, rows,
+            gemm_store_tiles<Out, 2, 2>(dst, &sh.a[0][0][0], wave, lane, sum, acc, (rg * GEMM_WIDE_WAVES + wr) * GEMM_ROWS, rows,
                              (tg * GEMM_WIDE_TOK_TILES + wt) * GEMM_TOKENS, n_tokens);
             return;
         }
@@ -867,14 +867,15 @@ __global__ __launch_bounds__(64 * GEMM_DECODE_WAVES) void gemm_decode_kernel(
     }
 }
 
-// The product over the decoded tiles, with the tile of gemm_wide_kernel: 256 rows x 128 tokens per workgroup of eight waves,
-// one chunk of 64 columns per step in quarters of one 16-byte word of every operand, three LDS buffers.  The same additions in
+// The product over the decoded tiles: 256 rows x 128 tokens per workgroup of eight waves, as in gemm_wide_kernel, or 192 x 128 where
+// that makes better rounds of workgroups (gemm_decoded_row_tiles), one chunk of 64 columns per step in quarters of one 16-byte
+// word of every operand, three LDS buffers.  The same additions in
 // the same order: where the columns are split alike, the results are gemm_wide_kernel's bit for bit.
 //   Operands go from memory to LDS without passing through registers (the tiles lie in memory as they lie in LDS: a wave's
-// request is 1024 bytes on either side), one row tile and a share of x per wave and chunk.  A step's one barrier stands in
+// request is 1024 bytes on either side), six of a chunk's 48 requests (192 rows: five of 40) per wave.  A step's one barrier stands in
 // front of its third quarter: by then every wave has its last words of the step's buffer in registers (operands are read two
-// quarters ahead), so chunk s + 3 may come into it, and has waited for its own share of chunk s + 1 (six requests; the six of
-// chunk s + 2 stay on their way), so what is left of the step can already ask for the next step's first words.  A request has
+// quarters ahead), so chunk s + 3 may come into it, and has waited for its own share of chunk s + 1 (its requests for chunk
+// s + 2 stay on their way), so what is left of the step can already ask for the next step's first words.  A request has
 // two steps' time.
 //   What bounds it (4096 columns of the result x 2000 tokens, chains of 11008): the matrix cores are busy 55 % of the time at the 1.96
 // GHz that the card holds meanwhile, the vector units 20 %; 1.1 PFLOP/s, where a large product of the library reaches 1.17 to
@@ -885,12 +886,13 @@ __global__ __launch_bounds__(64 * GEMM_DECODE_WAVES) void gemm_decode_kernel(
 //   Against bringing the operands in through registers, gradient calls whole, 11008 x 4096 with 2000 tokens 226 -> 213 us, 4096 x
 // 11008 248 -> 232, 22016 x 4096 with 4096 828 -> 782; with the barrier at the step's end, where a request has one step, 219 ->
 // 206 on one card and 800 -> 885 on the largest; 128 x 128 tiles in four waves, two workgroups a compute unit, 248; the waves in
-// two groups, one reading a whole chunk's operands while the other multiplies, 11008 x 4096 227 -> 249, 22016 x 4096 780 -> 865.
+// two groups, one reading a whole chunk's operands while the other multiplies, 11008 x 4096 227 -> 249, 22016 x 4096 780 -> 865; a fourth
+// buffer (192 rows) no difference.
 //   2000 tokens with a list, gemm_wide_kernel -> decoding and this (through registers): 4096 x 4096 127 -> 102 us, 12288 x 4096
 // 353 -> 252, 22016 x 4096 649 -> 482, 8192 x 28672 1305 -> 1042.
-constexpr int GEMM_WAIT_ALL_LDS = 0x0f70;        // s_waitcnt: no request on its way into LDS
-constexpr int GEMM_WAIT_BUT_6_AND_READS = 0x0076;  // all requests but the last six, and every LDS read
-constexpr int GEMM_WAIT_BUT_12 = 0x0f7c;
+// s_waitcnt: for all requests but the last n (bits 3:0 and 15:14), and with the mask for every LDS read as well (bits 11:8).
+constexpr int gemm_wait_but(int n) { return 0x0f70 | (n & 15) | ((n >> 4) << 14); }
+constexpr int GEMM_AND_LDS_READS = ~0x0f00;
 // A barrier that waits for nothing by itself; no memory access moves across it.
 __device__ __forceinline__ void gemm_bare_barrier() {
     asm volatile("" ::: "memory");
@@ -898,16 +900,16 @@ __device__ __forceinline__ void gemm_bare_barrier() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
-template <bool CARRY, class Out>
+template <bool CARRY, int ROW_TILES, class Out>
 __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
     const uint4* __restrict__ decoded, uint32_t first_row, uint32_t n_rt, uint32_t rows, uint32_t n_chunks,
     const uint4* __restrict__ xp, uint32_t tok_tiles, uint32_t tok_groups, uint32_t per_split, uint32_t flush,
     uint32_t n_tokens, uint32_t n_parts, Out dst) {
-    struct Shared {
-        uint4 a[3][GEMM_WIDE_WAVES][GEMM_TILE_WORDS];
-        uint4 b[3][GEMM_WIDE_TOK_TILES][GEMM_TILE_WORDS];
-    };
-    __shared__ __attribute__((aligned(16))) Shared sh;
+    static_assert(ROW_TILES == 8 || ROW_TILES == 6, "eight waves of 2 x 2 or of 3 x 1 tiles");
+    constexpr int RW = ROW_TILES == 8 ? 2 : 3, TW = ROW_TILES == 8 ? 2 : 1;  // a wave's row tiles and token tiles
+    constexpr uint32_t TILES = ROW_TILES + GEMM_WIDE_TOK_TILES;             // of a chunk, row tiles first
+    constexpr int REQUESTS = TILES * 4 / GEMM_WIDE_WAVES;                   // of a wave per chunk, 1024 bytes each
+    __shared__ __attribute__((aligned(16))) uint4 sh[3][TILES][GEMM_TILE_WORDS];
     const uint32_t tid = threadIdx.x, lane = tid & 63;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // As in gemm_wide_kernel each die takes a contiguous run of tiles; it goes through bands of four row groups, token group by
@@ -918,41 +920,50 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
         const uint32_t total = gridDim.x, q = total / 8, rem = total % 8, die = id % 8;
         id = die * q + min(die, rem) + id / 8;
     }
-    const uint32_t row_groups = (n_rt + GEMM_WIDE_WAVES - 1) / GEMM_WIDE_WAVES;
+    const uint32_t row_groups = (n_rt + ROW_TILES - 1) / ROW_TILES;
     const uint32_t part = id / (tok_groups * row_groups), place = id - part * tok_groups * row_groups;
     const uint32_t band = place / (4 * tok_groups), in_band = place - band * 4 * tok_groups, height = min(4u, row_groups - 4 * band);
     const uint32_t tg = in_band / height, rg = 4 * band + in_band % height;
     const uint32_t ch0 = part * per_split, ch1 = min(n_chunks, ch0 + per_split), n_steps = ch1 - ch0;
-    // a row tile or token tile past the last is read from the last one and not stored
-    const uint4* my_a = decoded + (uint64_t)min(rg * GEMM_WIDE_WAVES + wave, n_rt - 1) * n_chunks * GEMM_TILE_WORDS + lane;
-    const uint4* my_x = xp + (uint64_t)min(tg * GEMM_WIDE_TOK_TILES + (wave >> 1), tok_tiles - 1) * n_chunks * GEMM_TILE_WORDS +
-                        (wave & 1) * 128 + lane;
-    // The wave's share of a chunk, six requests; past the last chunk the last one again, so that there are always six.
+    // The wave's requests of a chunk: words 64 j .. + 63 of a tile each.  A row tile or token tile past the last is read from the
+    // last one and not stored.
+    const uint4* from[REQUESTS];
+#pragma unroll
+    for (int i = 0; i < REQUESTS; ++i) {
+        const uint32_t tile = (wave * REQUESTS + i) / 4, j = (wave * REQUESTS + i) % 4;
+        const uint4* tiles = tile < ROW_TILES ? decoded + (uint64_t)min(rg * ROW_TILES + tile, n_rt - 1) * n_chunks * GEMM_TILE_WORDS
+                                              : xp + (uint64_t)min(tg * GEMM_WIDE_TOK_TILES + tile - ROW_TILES, tok_tiles - 1) * n_chunks * GEMM_TILE_WORDS;
+        from[i] = tiles + 64 * j + lane;
+    }
+    // Past the last chunk the last one is asked for again, so that there are always as many requests.
     auto bring = [&](uint32_t nth, uint32_t buf) __attribute__((always_inline)) {
         const uint64_t at = (uint64_t)min(ch0 + nth, ch1 - 1) * GEMM_TILE_WORDS;
         typedef const __attribute__((address_space(1))) void* G;
         typedef __attribute__((address_space(3))) void* L;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) __builtin_amdgcn_global_load_lds((G)(my_a + at + 64 * j), (L)&sh.a[buf][wave][64 * j], 16, 0, 0);
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            __builtin_amdgcn_global_load_lds((G)(my_x + at + 64 * j), (L)&sh.b[buf][wave >> 1][(wave & 1) * 128 + 64 * j], 16, 0, 0);
+        for (int i = 0; i < REQUESTS; ++i)
+            __builtin_amdgcn_global_load_lds((G)(from[i] + at), (L)&sh[buf][0][(wave * REQUESTS + i) * 64], 16, 0, 0);
     };
-    gemm_f32x16 acc[2][2], sum[2][2];  // [row tile][token tile]
+    gemm_f32x16 acc[RW][TW], sum[RW][TW];  // [row tile][token tile]
 #pragma unroll
-    for (int r = 0; r < 2; ++r)
+    for (int r = 0; r < RW; ++r)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < TW; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[r][t][i] = sum[r][t][i] = 0.0f;
-    const uint32_t wr = 2 * (wave & 3), wt = 2 * (wave >> 2);  // first row tile and token tile that the wave multiplies
+    // first row tile and token tile that the wave multiplies
+    const uint32_t wr = ROW_TILES == 8 ? 2 * (wave & 3) : 3 * (wave & 1), wt = ROW_TILES == 8 ? 2 * (wave >> 2) : wave >> 1;
     struct Operands {
-        gemm_bf16x8 a[2], b[2];
+        gemm_bf16x8 a[RW], b[TW];
     };
     auto read_operands = [&](uint32_t buf, int j) __attribute__((always_inline)) {
-        const gemm_bf16x8* a = reinterpret_cast<const gemm_bf16x8*>(sh.a[buf][wr]) + lane;
-        const gemm_bf16x8* b = reinterpret_cast<const gemm_bf16x8*>(sh.b[buf][wt]) + lane;
-        const Operands o = {{a[64 * j], a[GEMM_TILE_WORDS + 64 * j]}, {b[64 * j], b[GEMM_TILE_WORDS + 64 * j]}};
+        const gemm_bf16x8* a = reinterpret_cast<const gemm_bf16x8*>(sh[buf][wr]) + lane;
+        const gemm_bf16x8* b = reinterpret_cast<const gemm_bf16x8*>(sh[buf][ROW_TILES + wt]) + lane;
+        Operands o;
+#pragma unroll
+        for (int r = 0; r < RW; ++r) o.a[r] = a[r * GEMM_TILE_WORDS + 64 * j];
+#pragma unroll
+        for (int t = 0; t < TW; ++t) o.b[t] = b[t * GEMM_TILE_WORDS + 64 * j];
         return o;
     };
     uint32_t until_flush = flush;
@@ -964,21 +975,21 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (j == 2) {
-                __builtin_amdgcn_s_waitcnt(GEMM_WAIT_BUT_6_AND_READS);
+                __builtin_amdgcn_s_waitcnt(gemm_wait_but(REQUESTS) & GEMM_AND_LDS_READS);
                 gemm_bare_barrier();
                 bring(s + 3, buf);
             }
             const Operands next = read_operands(j < 2 ? buf : buf1, (j + 2) & 3);
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
+            for (int r = 0; r < RW; ++r)
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < TW; ++t)
                     acc[r][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op.b[t], op.a[r], acc[r][t], 0, 0, 0);
             __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
             __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, RW * TW - 2, 0);
             __builtin_amdgcn_sched_barrier(0);
             op = op1;
             op1 = next;
@@ -986,9 +997,9 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
         if (--until_flush == 0u) {
             until_flush = flush;
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
+            for (int r = 0; r < RW; ++r)
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < TW; ++t)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         if (CARRY) {
@@ -1003,7 +1014,7 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
     bring(0, 0);
     bring(1, 1);
     bring(2, 2);
-    __builtin_amdgcn_s_waitcnt(GEMM_WAIT_BUT_12);
+    __builtin_amdgcn_s_waitcnt(gemm_wait_but(2 * REQUESTS));
     gemm_bare_barrier();
     op = read_operands(0, 0);
     op1 = read_operands(0, 1);
@@ -1017,22 +1028,22 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
         step(s, 0);
         if (s + 1 < n_steps) step(s + 1, 1);
     }
-    __builtin_amdgcn_s_waitcnt(GEMM_WAIT_ALL_LDS);  // (chunks past the last were asked for, too)
+    __builtin_amdgcn_s_waitcnt(gemm_wait_but(0));  // (chunks past the last were asked for, too)
     if constexpr (Out::LAYER) {
         if (n_parts == 1) {
-            gemm_store_tiles(dst, &sh.a[0][0][0], wave, lane, sum, acc, first_row + (rg * GEMM_WIDE_WAVES + wr) * GEMM_ROWS,
-                             min(rows, first_row + n_rt * GEMM_ROWS),
-                             (tg * GEMM_WIDE_TOK_TILES + wt) * GEMM_TOKENS, n_tokens);
+            gemm_store_tiles<Out, RW, TW>(dst, &sh[0][0][0], wave, lane, sum, acc, first_row + (rg * ROW_TILES + wr) * GEMM_ROWS,
+                                          min(rows, first_row + n_rt * GEMM_ROWS), (tg * GEMM_WIDE_TOK_TILES + wt) * GEMM_TOKENS,
+                                          n_tokens);
             return;
         }
     }
     // the first part of a plain product goes to the result itself, where gemm_sum_kernel adds the others to it
     float* out = dst.part(part, n_tokens, rows);
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const uint32_t rt = rg * GEMM_WIDE_WAVES + wr + r, row = first_row + rt * GEMM_ROWS + (lane & 31);
+    for (int r = 0; r < RW; ++r) {
+        const uint32_t rt = rg * ROW_TILES + wr + r, row = first_row + rt * GEMM_ROWS + (lane & 31);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < TW; ++t) {
             const uint32_t tok0 = (tg * GEMM_WIDE_TOK_TILES + wt + t) * GEMM_TOKENS + 4 * (lane >> 5);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -1042,7 +1053,6 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
         }
     }
 }
-
 
 // y = the partial results in order (count elements each): the first, which may stand in y itself, and n_more others.
 static __global__ __launch_bounds__(256) void gemm_sum_kernel(const float* first, const float* __restrict__ more, uint32_t n_more,

@@ -185,6 +185,16 @@ inline GemmDecodedPlan gemm_decoded_plan(uint64_t rows, uint64_t cols, uint64_t 
     best.time += 6.0 + 0.8e-6 * (double)(tok_tiles * GEMM_TOKENS * cols);
     return best;
 }
+// Row tiles of a workgroup of gemm_decoded_kernel for a slab of n_rt of them, with `others` workgroups along tokens and columns and
+// `per` chunks each: eight, or six where the workgroups' rounds of 256 take less time so (the sums are the same bit for bit).
+// Eight / six, layers without a list, us: 12288 x 4096 with 700 tokens (two rounds either way) 142 / 119, 11008 x 4096 with 1000 143 /
+// 125, 4096 x 4096 with 2000 (one round / two) 88 / 111, 22016 x 4096 with 4096 755 / 795.  Over 70 gradient calls of 500 to 16000
+// rows, 512 to 14000 columns and 40 to 3000 tokens the rule's choice is 6 % faster than eight in the mean (up to 19 %) and at
+// most 2 % slower than the better of the two.
+inline uint32_t gemm_decoded_row_tiles(uint64_t n_rt, uint64_t others, uint64_t per) {
+    const double rounds8 = (double)(((n_rt + 7) / 8 * others + 255) / 256), rounds6 = (double)(((n_rt + 5) / 6 * others + 255) / 256);
+    return rounds6 * (7.0 + 0.65 * (double)per) < rounds8 * (7.5 + 0.82 * (double)per) ? 6 : 8;
+}
 // The plan where the product is decoded first, else slab_tiles = 0.  W: gemm_wide_choice's answer.
 inline GemmDecodedPlan gemm_decoded_choice(uint64_t rows, uint64_t cols, uint64_t tok_tiles, bool list, const GemmWideSplit& W) {
     const GemmDecodedPlan no = {0, 0, 0, 0.0, 0, 0, false};

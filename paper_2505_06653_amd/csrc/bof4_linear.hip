@@ -176,7 +176,6 @@ int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t co
     uint4* decoded = (uint4*)(ws + P.decoded);
     const uint32_t row_chunks = (uint32_t)((rows + GEMM_CHUNK - 1) / GEMM_CHUNK), chunks = (uint32_t)((cols + GEMM_CHUNK - 1) / GEMM_CHUNK);
     const uint32_t tok_tiles = (n_tokens + GEMM_TOKENS - 1) / GEMM_TOKENS;
-    const uint32_t tok_groups = (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES;
     const LinearGradArgs a = {l.dy_dev, l.act != ACT_NONE || l.dmul_dev ? l.pre_dev : nullptr, l.mul_dev, l.dmul_dev,
                               l.dbias_dev ? dbias_parts : nullptr, l.ld_dy, l.ld_pre, l.ld_mul, l.ld_dmul, l.act,
                               l.dy_type == BOF4_BF16, l.pre_type == BOF4_BF16, l.mul_type == BOF4_BF16, l.dmul_type == BOF4_BF16};
@@ -202,7 +201,6 @@ int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t co
     for (uint32_t ct0 = 0; ct0 < col_tiles; ct0 += D.slab_tiles) {
         const uint32_t n_ct = col_tiles - ct0 < D.slab_tiles ? col_tiles - ct0 : D.slab_tiles;
         const uint64_t jobs = (uint64_t)((n_ct + 1) / 2) * row_chunks;
-        const uint32_t groups = (n_ct + GEMM_WIDE_WAVES - 1) / GEMM_WIDE_WAVES;
         const LinearDzCall dz = {a, ct0 == 0 && !dz_apart ? row_chunks * P.ranges : 0, n_tokens, (uint32_t)rows, tok_tiles, P.tiles_per_range, xp};
 #define BOF4_LAUNCH_TURN(OUT_)                                                                                          \
     hipLaunchKernelGGL((linear_turn_kernel<OUT_>),                                                                      \
@@ -211,9 +209,7 @@ int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t co
                        offsets_dev, entries_dev, (uint32_t)n_outliers, T.lg, T.row_tiles, decoded, dz);
         if (n_outliers > 0) { BOF4_LAUNCH_TURN(true) } else { BOF4_LAUNCH_TURN(false) }
 #undef BOF4_LAUNCH_TURN
-        hipLaunchKernelGGL((gemm_decoded_kernel<false, LayerOut>), dim3(tok_groups * groups * D.split), dim3(64 * GEMM_WIDE_WAVES),
-                           0, s, decoded, ct0 * GEMM_ROWS, n_ct, (uint32_t)cols, row_chunks, xp, tok_tiles, tok_groups, D.per_split,
-                           FLUSH, n_tokens, D.split, out);
+        gemm_multiply_decoded(D, FLUSH, false, decoded, ct0 * GEMM_ROWS, n_ct, cols, row_chunks, xp, n_tokens, out, s);
     }
     const uint32_t dbias_groups = l.dbias_dev ? (uint32_t)((rows + 255) / 256) : 0;
     if (D.split > 1) {

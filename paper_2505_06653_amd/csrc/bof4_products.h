@@ -118,6 +118,25 @@ void gemm_add_parts(uint32_t split, uint32_t n_tokens, uint64_t rows, const Out&
     }
 }
 
+// A slab of the decoded matrix times x, with 256 or 192 rows to a workgroup.
+template <class Out>
+void gemm_multiply_decoded(const GemmDecodedPlan& D, uint32_t flush, bool carry, const uint4* decoded, uint32_t first_row, uint32_t n_rt,
+                           uint64_t rows, uint32_t chunks, const uint4* xp, uint32_t n_tokens, const Out& dst, hipStream_t s) {
+    const uint32_t tok_tiles = (n_tokens + GEMM_TOKENS - 1) / GEMM_TOKENS;
+    const uint32_t tok_groups = (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES;
+    const uint32_t tiles = gemm_decoded_row_tiles(n_rt, tok_groups * D.split, D.per_split), groups = (n_rt + tiles - 1) / tiles;
+#define BOF4_LAUNCH_DECODED(CARRY_, TILES_)                                                                                  \
+    hipLaunchKernelGGL((gemm_decoded_kernel<CARRY_, TILES_, Out>), dim3(tok_groups * groups * D.split), dim3(64 * GEMM_WIDE_WAVES), \
+                       0, s, decoded, first_row, n_rt, (uint32_t)rows, chunks, xp, tok_tiles, tok_groups, D.per_split, flush,  \
+                       n_tokens, D.split, dst);
+    if (tiles == 8) {
+        if (carry) { BOF4_LAUNCH_DECODED(true, 8) } else { BOF4_LAUNCH_DECODED(false, 8) }
+    } else {
+        if (carry) { BOF4_LAUNCH_DECODED(true, 6) } else { BOF4_LAUNCH_DECODED(false, 6) }
+    }
+#undef BOF4_LAUNCH_DECODED
+}
+
 struct GemmCall {
     const void* packed_dev;
     uint64_t rows, cols;
@@ -161,20 +180,14 @@ int gemm_run(const GemmCall& call, const GemmPlan& P, Out dst) {
         for (uint32_t rt0 = 0; rt0 < T.row_tiles; rt0 += D.slab_tiles) {
             const uint32_t n_rt = T.row_tiles - rt0 < D.slab_tiles ? T.row_tiles - rt0 : D.slab_tiles;
             const uint64_t jobs = (uint64_t)n_rt * ((chunks + GEMM_DECODE_TILES - 1) / GEMM_DECODE_TILES);
-            const uint32_t groups = (n_rt + GEMM_WIDE_WAVES - 1) / GEMM_WIDE_WAVES;
             const uint32_t packing = rt0 == 0 ? pack_groups : 0, decoding = (uint32_t)((jobs + GEMM_DECODE_WAVES - 1) / GEMM_DECODE_WAVES);
 #define BOF4_LAUNCH_DECODE(OUT_)                                                                                       \
     hipLaunchKernelGGL((gemm_decode_kernel<OUT_>), dim3(packing + decoding), dim3(64 * GEMM_DECODE_WAVES), 0, s,       \
                        (const char*)packed_dev, rt0, n_rt, chunks, cb, offsets_dev, entries_dev, (uint32_t)n_outliers, T.lg, \
                        T.row_tiles, decoded, packing, (const uint16_t*)x_dev, n_tokens, (uint32_t)cols, n_pad, (uint4*)xp);
-#define BOF4_LAUNCH_DECODED(CARRY_)                                                                                    \
-    hipLaunchKernelGGL((gemm_decoded_kernel<CARRY_, Out>), dim3(tok_groups * groups * D.split), dim3(64 * GEMM_WIDE_WAVES), \
-                       0, s, decoded, rt0 * GEMM_ROWS, n_rt, (uint32_t)rows, chunks, xp, tok_tiles, tok_groups,        \
-                       D.per_split, D.flush, n_tokens, D.split, dst);
             if (n_outliers > 0) { BOF4_LAUNCH_DECODE(true) } else { BOF4_LAUNCH_DECODE(false) }
-            if (D.carry) { BOF4_LAUNCH_DECODED(true) } else { BOF4_LAUNCH_DECODED(false) }
+            gemm_multiply_decoded(D, D.flush, D.carry, decoded, rt0 * GEMM_ROWS, n_rt, rows, chunks, xp, n_tokens, dst, s);
 #undef BOF4_LAUNCH_DECODE
-#undef BOF4_LAUNCH_DECODED
         }
         if (D.split > 1) gemm_add_parts(D.split, n_tokens, rows, dst, s);
         timing_end(s);
