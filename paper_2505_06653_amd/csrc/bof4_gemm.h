@@ -868,7 +868,7 @@ __global__ __launch_bounds__(64 * GEMM_DECODE_WAVES) void gemm_decode_kernel(
 }
 
 // The product over the decoded tiles: 256 rows x 128 tokens per workgroup of eight waves, as in gemm_wide_kernel, or 192 x 128 where
-// that makes better rounds of workgroups (gemm_decoded_row_tiles), one chunk of 64 columns per step in quarters of one 16-byte
+// that makes better rounds of workgroups (gemm_decoded_tile), one chunk of 64 columns per step in quarters of one 16-byte
 // word of every operand, three LDS buffers.  The same additions in
 // the same order: where the columns are split alike, the results are gemm_wide_kernel's bit for bit.
 //   Operands go from memory to LDS without passing through registers (the tiles lie in memory as they lie in LDS: a wave's

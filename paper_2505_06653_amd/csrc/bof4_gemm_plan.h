@@ -153,6 +153,23 @@ inline GemmChains gemm_chains(uint64_t rows, uint64_t cols, uint64_t n_tokens, b
 //   without a list   4096 x 4096, 512 / 1000 / 2000 tokens 45 / 67 / 103 -> 48 / 66 / 93, 12288 x 4096 86 / 174 / 286 -> 85 /
 //                    151 / 236, 22016 x 4096 172 / 273 / 522 -> 162 / 239 / 442, 8192 x 28672 297 / 569 / 1185 -> 362 / 557 / 1020
 constexpr uint64_t GEMM_DECODED_BYTES = 256ull << 20;
+
+// Row tiles of a workgroup of gemm_decoded_kernel for a slab of n_rt of them, with `others` workgroups along tokens and columns and
+// `per` chunks each: eight, or six where the workgroups' rounds of 256 take less time so (the sums are the same bit for bit).
+// Eight / six, layers without a list, us: 12288 x 4096 with 700 tokens (two rounds either way) 142 / 119, 11008 x 4096 with 1000 143 /
+// 125, 4096 x 4096 with 2000 (one round / two) 88 / 111, 22016 x 4096 with 4096 755 / 795.  Over 70 gradient calls of 500 to 16000
+// rows, 512 to 14000 columns and 40 to 3000 tokens the rule's choice is 6 % faster than eight in the mean (up to 19 %) and at
+// most 2 % slower than the better of the two.
+struct GemmDecodedTile {
+    uint32_t row_tiles;
+    double time;
+};
+inline GemmDecodedTile gemm_decoded_tile(uint64_t n_rt, uint64_t others, uint64_t per) {
+    const double time8 = (double)(((n_rt + 7) / 8 * others + 255) / 256) * (7.5 + 0.82 * (double)per);
+    const double time6 = (double)(((n_rt + 5) / 6 * others + 255) / 256) * (7.0 + 0.65 * (double)per);
+    return time6 < time8 ? GemmDecodedTile{6, time6} : GemmDecodedTile{8, time8};
+}
+
 struct GemmDecodedPlan {
     uint32_t slab_tiles;        // row tiles per slab, 0: not this way
     uint32_t split, per_split;  // workgroups along the columns, chunks each
@@ -161,7 +178,9 @@ struct GemmDecodedPlan {
     uint32_t flush;  // chunks in one chain of additions
     bool carry;
 };
-inline GemmDecodedPlan gemm_decoded_plan(uint64_t rows, uint64_t cols, uint64_t tok_tiles) {
+// `layer`: by the time of the tile that gemm_decoded_tile picks.  (A plain product's splits and slabs stay as the 256 x 128 tile
+// wants them, and with them the order of its additions.)
+inline GemmDecodedPlan gemm_decoded_plan(uint64_t rows, uint64_t cols, uint64_t tok_tiles, bool layer = false) {
     const uint64_t tok_groups = (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES;
     const uint64_t groups = (rows + GEMM_WIDE_WAVES * GEMM_ROWS - 1) / (GEMM_WIDE_WAVES * GEMM_ROWS);
     const uint64_t chunks = (cols + GEMM_CHUNK - 1) / GEMM_CHUNK, slots = tok_groups * GEMM_WIDE_TOK_TILES * GEMM_TOKENS;
@@ -176,7 +195,10 @@ inline GemmDecodedPlan gemm_decoded_plan(uint64_t rows, uint64_t cols, uint64_t 
             const double sums = split > 1 ? 2.0 + (double)((2 * split + 1) * slots * rows) * 4.0 / 7e6 : 0.0;
             if (best.slab_tiles != 0 && sums >= best.time) break;  // (more in every wider split)
             const uint64_t rounds = (n_slabs - 1) * ((slab * tok_groups * split + 255) / 256) + (last * tok_groups * split + 255) / 256;
-            const double time = sums + 4.0 * (double)n_slabs + (double)rounds * (7.5 + 0.82 * (double)per) +
+            const double whole = gemm_decoded_tile(slab * GEMM_WIDE_WAVES, tok_groups * split, per).time;
+            const double rest = gemm_decoded_tile(last * GEMM_WIDE_WAVES, tok_groups * split, per).time;
+            const double products = layer ? (double)(n_slabs - 1) * whole + rest : (double)rounds * (7.5 + 0.82 * (double)per);
+            const double time = sums + 4.0 * (double)n_slabs + products +
                                 (slab * group_bytes > (200ull << 20) ? 0.9e-6 : 0.46e-6) * (double)(rows * cols);
             if (best.slab_tiles == 0 || time < best.time)
                 best = {(uint32_t)(slab * GEMM_WIDE_WAVES), (uint32_t)split, (uint32_t)per, time, (size_t)(slab * group_bytes), 0, false};
@@ -184,16 +206,6 @@ inline GemmDecodedPlan gemm_decoded_plan(uint64_t rows, uint64_t cols, uint64_t 
     }
     best.time += 6.0 + 0.8e-6 * (double)(tok_tiles * GEMM_TOKENS * cols);
     return best;
-}
-// Row tiles of a workgroup of gemm_decoded_kernel for a slab of n_rt of them, with `others` workgroups along tokens and columns and
-// `per` chunks each: eight, or six where the workgroups' rounds of 256 take less time so (the sums are the same bit for bit).
-// Eight / six, layers without a list, us: 12288 x 4096 with 700 tokens (two rounds either way) 142 / 119, 11008 x 4096 with 1000 143 /
-// 125, 4096 x 4096 with 2000 (one round / two) 88 / 111, 22016 x 4096 with 4096 755 / 795.  Over 70 gradient calls of 500 to 16000
-// rows, 512 to 14000 columns and 40 to 3000 tokens the rule's choice is 6 % faster than eight in the mean (up to 19 %) and at
-// most 2 % slower than the better of the two.
-inline uint32_t gemm_decoded_row_tiles(uint64_t n_rt, uint64_t others, uint64_t per) {
-    const double rounds8 = (double)(((n_rt + 7) / 8 * others + 255) / 256), rounds6 = (double)(((n_rt + 5) / 6 * others + 255) / 256);
-    return rounds6 * (7.0 + 0.65 * (double)per) < rounds8 * (7.5 + 0.82 * (double)per) ? 6 : 8;
 }
 // The plan where the product is decoded first, else slab_tiles = 0.  W: gemm_wide_choice's answer.
 inline GemmDecodedPlan gemm_decoded_choice(uint64_t rows, uint64_t cols, uint64_t tok_tiles, bool list, const GemmWideSplit& W) {
@@ -234,6 +246,22 @@ inline GemmDecodedPlan gemm_decoded_choice(uint64_t rows, uint64_t cols, uint64_
     return (kind ? 1.03 : 0.98) * D.time * cost + 1.0 < other ? D : no;
 }
 
+// The same for a layer whose results are all rounded to bfloat16: decoded first wherever that is faster (gemm_plan says why the
+// chains of additions need no care there).  The models put decoding first 3 to 30 % too high on layers, and the other kernels 10 %
+// too low with a list.  Other kernel / decoded first, us: 11008 x 4096 with 300 tokens 88 / 69, 22016 x 4096 with 500 175 / 146 and
+// with a list and 300 177 / 137, 8192 x 8192 with 300 98 / 92, but 4096 x 11008 with 300 59 / 69 and 4096 x 4096 with 256 37 / 39.
+// Over 172 layers of 1000 to 28672 rows, 1024 to 16640 columns and 130 to 4000 tokens this choice is 0.95 to 1.24 times as fast
+// as gemm_decoded_choice's, 1.2 % faster in the mean; over 180 of 64 to 2500 rows and 512 to 2560 columns 0.92 to 1.47, 10 %.
+inline GemmDecodedPlan gemm_decoded_choice_bf16(uint64_t rows, uint64_t cols, uint64_t tok_tiles, bool list, const GemmWideSplit& W) {
+    const GemmDecodedPlan no = {0, 0, 0, 0.0, 0, 0, false};
+    const uint64_t wg_rows = GEMM_WIDE_WAVES * GEMM_ROWS, tok_groups = (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES;
+    if (tok_groups < 2 || cols < 512 || cols > GEMM_MAX_COLS || (rows + wg_rows - 1) / wg_rows * tok_groups >= (1ull << 23)) return no;
+    const double other = (list ? 1.1 : 1.0) * (W.split > 0 ? W.time : gemm_kernel_time(rows, cols, tok_tiles));
+    if (0.95 * (10.0 + 0.46e-6 * (double)(rows * cols)) >= other) return no;  // (no plan is shorter)
+    const GemmDecodedPlan D = gemm_decoded_plan(rows, cols, tok_tiles, true);
+    return 0.95 * D.time < other ? D : no;
+}
+
 // Workspace of bof4_gemm: x in the order of the products, then the partial results of the workgroups that share a row.
 // gemm_kernel's lie behind `part`; the wide kernel's - all but the first part's, which goes to y - behind `wide_part`.
 // `total` is what a call cannot do without and what gemm_kernel takes; it holds room for a second copy of x that only the
@@ -266,14 +294,15 @@ inline GemmWsLayout gemm_ws_layout(uint64_t rows, uint64_t cols, uint64_t n_toke
 // tokens).  Splits and slabs are the same for all token tiles of a group, so the most tokens of a group for which a kernel is
 // chosen need the most: 8192 x 28672 at 2000 / 65536 tokens 29 us / 0.37 ms, 4096 x 4096 15 us / 0.18 ms (45 / 1500 and 30 / 1000
 // where every token tile is asked about).
+// A layer's covers both types of results.
 inline size_t gemm_ws_bytes(uint64_t rows, uint64_t cols, uint64_t n_tokens, bool layer = false) {
     size_t need = gemm_ws_layout(rows, cols, n_tokens).total;
     const uint64_t most = n_tokens < GEMM_MAX_TOKENS ? n_tokens : GEMM_MAX_TOKENS;
     const uint64_t all_tiles = (most + GEMM_TOKENS - 1) / GEMM_TOKENS;
     for (uint64_t below = 0; below < all_tiles; below += GEMM_WIDE_TOK_TILES) {  // the token tiles before a group
-        bool has_wide = false, has_decoded = false;
+        bool has_wide = false, has_decoded = false, has_bf16 = !layer;
         for (uint64_t tiles = below + GEMM_WIDE_TOK_TILES < all_tiles ? below + GEMM_WIDE_TOK_TILES : all_tiles;
-             tiles > below && !(has_wide && has_decoded); --tiles) {
+             tiles > below && !(has_wide && has_decoded && has_bf16); --tiles) {
             const uint64_t t = tiles * GEMM_TOKENS < most ? tiles * GEMM_TOKENS : most;  // the most tokens in them
             for (const bool list : {true, false}) {  // (which kernel is chosen depends on it, neither way the other's superset)
                 const GemmWideSplit W = gemm_wide_choice(rows, cols, tiles, list);
@@ -282,12 +311,16 @@ inline size_t gemm_ws_bytes(uint64_t rows, uint64_t cols, uint64_t n_tokens, boo
                     if (bytes > need) need = bytes;
                     has_wide = true;
                 }
-                if (has_decoded) continue;
-                const GemmDecodedPlan D = gemm_decoded_choice(rows, cols, tiles, list, W);
-                if (D.slab_tiles == 0) continue;
-                const size_t bytes = gemm_ws_layout(rows, cols, t).decoded(D.split, t, rows, layer) + D.slab_bytes;
-                if (bytes > need) need = bytes;
-                has_decoded = true;
+                for (const bool bf16 : {false, true}) {
+                    bool& has = bf16 ? has_bf16 : has_decoded;
+                    if (has) continue;
+                    const GemmDecodedPlan D = bf16 ? gemm_decoded_choice_bf16(rows, cols, tiles, list, W)
+                                                   : gemm_decoded_choice(rows, cols, tiles, list, W);
+                    if (D.slab_tiles == 0) continue;
+                    const size_t bytes = gemm_ws_layout(rows, cols, t).decoded(D.split, t, rows, layer) + D.slab_bytes;
+                    if (bytes > need) need = bytes;
+                    has = true;
+                }
             }
         }
     }
@@ -305,13 +338,25 @@ struct GemmPlan {
     GemmChains chains;
     bool x_in_place;
 };
-inline GemmPlan gemm_plan(uint64_t rows, uint64_t cols, uint64_t n_tokens, bool list, size_t ws_bytes, bool layer = false) {
+// A layer whose results are all rounded to bfloat16 (`bf16`) needs none of what keeps the last bits of the sums: chains of 512
+// columns in the kernels with 256 x 128 tiles, uncut ones in gemm_kernel.  Their error, some 10^-7 of the sums, is below a
+// ten-thousandth of the results' rounding.  With a list: 11008 x 4096, 500 tokens, the product 87 -> 73 us.
+enum GemmResults { GEMM_PLAIN, GEMM_LAYER, GEMM_LAYER_BF16 };
+inline GemmPlan gemm_plan(uint64_t rows, uint64_t cols, uint64_t n_tokens, bool list, size_t ws_bytes, GemmResults results = GEMM_PLAIN) {
     const uint64_t tok_tiles = (n_tokens + GEMM_TOKENS - 1) / GEMM_TOKENS;
+    const bool layer = results != GEMM_PLAIN, bf16 = results == GEMM_LAYER_BF16;
     GemmPlan P;
     P.ws = gemm_ws_layout(rows, cols, n_tokens);
     P.wide = gemm_wide_choice(rows, cols, tok_tiles, list);
-    P.decoded = gemm_decoded_choice(rows, cols, tok_tiles, list, P.wide);
+    P.decoded = bf16 ? gemm_decoded_choice_bf16(rows, cols, tok_tiles, list, P.wide)
+                     : gemm_decoded_choice(rows, cols, tok_tiles, list, P.wide);
     P.chains = gemm_chains(rows, cols, n_tokens, list);
+    if (bf16) {
+        P.chains.list_flush = 0xffffffffu;
+        P.chains.n_runs = 1;
+        P.chains.wide_flush = P.decoded.flush = 8;
+        P.chains.wide_carry = P.decoded.carry = false;
+    }
     P.x_in_place = P.wide.split == 0 && gemm_x_in_place(rows, cols, n_tokens, list);
     P.way = GEMM_NARROW;
     if (P.decoded.slab_tiles > 0 && ws_bytes >= P.ws.decoded(P.decoded.split, n_tokens, rows, layer) + P.decoded.slab_bytes)
@@ -319,16 +364,6 @@ inline GemmPlan gemm_plan(uint64_t rows, uint64_t cols, uint64_t n_tokens, bool 
     else if (P.wide.split > 0 && ws_bytes >= P.ws.wide(P.wide.split, n_tokens, rows, layer))
         P.way = GEMM_WIDE;
     return P;
-}
-
-// A layer whose results are all rounded to bfloat16 needs none of what keeps the last bits of the sums: chains of 512 columns
-// in the 256 x 128 tile, uncut ones in gemm_kernel.  Their error, some 10^-7 of the sums, is below a ten-thousandth of the
-// results' rounding.  With a list: 11008 x 4096, 500 tokens, the product 87 -> 73 us.
-inline void gemm_plan_for_bf16(GemmPlan& P) {
-    P.chains.list_flush = 0xffffffffu;
-    P.chains.n_runs = 1;
-    P.chains.wide_flush = P.decoded.flush = 8;
-    P.chains.wide_carry = P.decoded.carry = false;
 }
 
 }  // namespace bof4

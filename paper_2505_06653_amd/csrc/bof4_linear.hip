@@ -124,8 +124,8 @@ int bof4_gemm_linear(const void* packed_dev, uint64_t rows, uint64_t cols, const
     LayerOut out;
     const int rc = layer_out(layer, rows, x_dev, &out);
     if (rc != BOF4_OK) return rc;
-    GemmPlan P = gemm_plan(rows, cols, n_tokens, n_outliers > 0, ws_bytes, true);
-    if (out.y_bf16 && (!out.pre || out.pre_bf16)) gemm_plan_for_bf16(P);
+    const GemmPlan P = gemm_plan(rows, cols, n_tokens, n_outliers > 0, ws_bytes,
+                                 out.y_bf16 && (!out.pre || out.pre_bf16) ? GEMM_LAYER_BF16 : GEMM_LAYER);
     if (ws_bytes < P.ws.total) return fail(BOF4_ERR_WORKSPACE, "bof4_gemm_linear: workspace too small");
     return gemm_run({packed_dev, rows, cols, cb_host, table_dev, n_outliers, x_dev, n_tokens, ws_dev, (hipStream_t)stream}, P, out);
 }

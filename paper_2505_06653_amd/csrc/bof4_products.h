@@ -124,7 +124,7 @@ void gemm_multiply_decoded(const GemmDecodedPlan& D, uint32_t flush, bool carry,
                            uint64_t rows, uint32_t chunks, const uint4* xp, uint32_t n_tokens, const Out& dst, hipStream_t s) {
     const uint32_t tok_tiles = (n_tokens + GEMM_TOKENS - 1) / GEMM_TOKENS;
     const uint32_t tok_groups = (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES;
-    const uint32_t tiles = gemm_decoded_row_tiles(n_rt, tok_groups * D.split, D.per_split), groups = (n_rt + tiles - 1) / tiles;
+    const uint32_t tiles = gemm_decoded_tile(n_rt, tok_groups * D.split, D.per_split).row_tiles, groups = (n_rt + tiles - 1) / tiles;
 #define BOF4_LAUNCH_DECODED(CARRY_, TILES_)                                                                                  \
     hipLaunchKernelGGL((gemm_decoded_kernel<CARRY_, TILES_, Out>), dim3(tok_groups * groups * D.split), dim3(64 * GEMM_WIDE_WAVES), \
                        0, s, decoded, first_row, n_rt, (uint32_t)rows, chunks, xp, tok_tiles, tok_groups, D.per_split, flush,  \

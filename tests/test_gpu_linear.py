@@ -536,3 +536,14 @@ def test_a_gated_block_and_its_answers_forward_and_back():
     # seven tensors in bfloat16 (u, pre, h, y, d_logits, dy, dh and du) of half a step, 2^-9 in the mean, and dz four times:
     # under sixteen such roundings, which the activations' slopes and the softmax pass on by at most a few times
     assert off(lp, lp_r.detach()) < 16 * 2.0 ** -9 and off(dx, want_dx) < 48 * 2.0 ** -9 and off(dbias, want_db) < 48 * 2.0 ** -9
+
+
+# (with results in bfloat16 these are decoded first, in workgroups of 192 rows, the columns whole or shared by 2, 4 and 8)
+@pytest.mark.parametrize("rows,cols,n_tokens,share", [(500, 544, 261, 0.0), (1000, 544, 333, 0.01), (500, 1056, 390, 0.01),
+                                                      (500, 2080, 261, 0.02), (500, 4128, 200, 0.01)])
+def test_gemm_linear_decoded_first_for_results_in_bfloat16(rows, cols, n_tokens, share):
+    m = Matrix(rows, cols, share)
+    bf16, f32 = torch.bfloat16, torch.float32
+    check(m, "gemm", n_tokens, "none")
+    check(m, "gemm", n_tokens, "silu", mul=f32, pre=bf16)
+    check(m, "gemm", n_tokens, "relu", bias=bf16, mul=bf16, residual=f32)
