@@ -815,24 +815,20 @@ def bof4_token_logprobs(logits, targets=None, top=0, ws=None, stream=None):
     if logits.dim() != 2:
         raise ValueError("logits must be [n_rows, vocab]")
     n, vocab = logits.shape
-    dev, f32, top = logits.device, torch.float32, int(top)
+    f32, top, new = torch.float32, int(top), logits.new_empty
     if top < 0:
         raise ValueError("top must not be negative")
     logprob = top_idx = top_logprob = targets_at = logprob_at = idx_at = top_at = None
-    # (one piece of memory for what is float32: a tensor of its own for each costs a call 1 us more)
-    both = torch.empty(n * (4 + top), dtype=f32, device=dev)
-    at = both.data_ptr()
-    stats, entropy = both.as_strided((n, 2), (2, 1), 0), both.as_strided((n,), (1,), 2 * n)
+    stats, entropy = new((n, 2), dtype=f32), new(n, dtype=f32)
     if targets is not None:
-        targets_at, logprob_at = _flat(targets, "targets", _I64, (n,), gpu), at + 12 * n
-        logprob = both.as_strided((n,), (1,), 3 * n)
+        targets_at, logprob = _flat(targets, "targets", _I64, (n,), gpu), new(n, dtype=f32)
+        logprob_at = logprob.data_ptr()
     if top > 0:
-        top_idx = torch.empty((n, top), dtype=torch.int64, device=dev)
-        top_logprob = both.as_strided((n, top), (top, 1), 4 * n)
-        idx_at, top_at = top_idx.data_ptr(), at + 16 * n
-    ws = _scratch(ws, 0 if ws is not None else bof4_token_logprobs_workspace_bytes(n, vocab, top), dev, stream)
+        top_idx, top_logprob = new((n, top), dtype=torch.int64), new((n, top), dtype=f32)
+        idx_at, top_at = top_idx.data_ptr(), top_logprob.data_ptr()
+    ws = _scratch(ws, 0 if ws is not None else bof4_token_logprobs_workspace_bytes(n, vocab, top), logits.device, stream)
     _check(lib().bof4_token_logprobs(logits_at, _TYPES[logits.dtype], n, vocab, _row_stride(logits), targets_at, top,
-                                     logprob_at, at + 8 * n, idx_at, top_at, at, ws.data_ptr(),
+                                     logprob_at, entropy.data_ptr(), idx_at, top_at, stats.data_ptr(), ws.data_ptr(),
                                      ws.numel(), _stream(stream)))
     return logprob, entropy, top_idx, top_logprob, stats
 

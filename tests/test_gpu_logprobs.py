@@ -335,3 +335,29 @@ def test_refusals():
         binding.bof4_token_logprobs_backward(x, stats, entropy=h)
     with pytest.raises(ValueError):
         binding.bof4_token_logprobs_backward(x, stats[:2], t, h)
+
+
+def test_results_changed_in_place_leave_what_the_gradient_needs():
+    """Inside an autograd function: the caller masks the log probabilities in place, the statistics stay as they were saved."""
+    class LogProb(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, t):
+            logprob, entropy, _, top, stats = binding.bof4_token_logprobs(x, t, top=3)
+            assert not any(r._is_view() for r in (logprob, entropy, top, stats))
+            ctx.save_for_backward(x, stats, t, entropy)
+            return logprob
+
+        @staticmethod
+        def backward(ctx, g):
+            x, stats, t, entropy = ctx.saved_tensors
+            return binding.bof4_token_logprobs_backward(x, stats, t, g.contiguous()), None
+
+    x = make(6, 1000, torch.float32, 3)[0].requires_grad_(True)
+    t = torch.arange(6, device=DEV) * 150
+    keep = torch.tensor([1.0, 0.0, 2.0, 1.0, 0.0, 1.0], device=DEV)
+    logprob = LogProb.apply(x, t)
+    logprob *= keep
+    logprob.sum().backward()
+    want = keep[:, None].double() * (torch.nn.functional.one_hot(t, 1000) - torch.softmax(x.detach().double(), -1))
+    # exp of a difference rounded at 2^-24 of up to 30, and the sum's own error: below 64 half steps of the largest gradient
+    assert float((x.grad.double() - want).abs().max()) <= 64 * 2.0 ** -24 * 2
