@@ -388,7 +388,8 @@ size_t bof4_gemm_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t n_tokens
 #define BOF4_ACT_GELU_TANH 3u /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
 #define BOF4_ACT_SILU 4u      /* z / (1 + exp(-z)) */
 /* What belongs to a layer besides the matrix (host struct, read during the call).  Types are BOF4_F32 or BOF4_BF16; ld_* are
- * elements from one token to the next (>= rows); every pointer has its element's alignment. */
+ * elements from one token to the next (>= rows); every pointer has its element's alignment.  What is written overlaps nothing
+ * else that the call reads or writes, but for the tensors named here, as a whole. */
 typedef struct {
     uint32_t act;                                               /* BOF4_ACT_*                                        */
     uint32_t bias_type, mul_type, residual_type, y_type, pre_type;
@@ -404,7 +405,8 @@ int bof4_gemv_linear(const uint8_t* codes_dev, const uint16_t* scales_dev, uint6
                      const double* cb_host, const void* table_dev, uint64_t n_outliers, const void* x_dev, uint32_t n_tokens,
                      const bof4_layer* layer, void* stream);
 /* bof4_gemm's arguments with the layer in the place of y, and its limits but 2^30 rows; the workspace is
- * bof4_gemm_linear_workspace_bytes(rows, cols, n_tokens), which never falls as n_tokens rises.  Only enqueues. */
+ * bof4_gemm_linear_workspace_bytes(rows, cols, n_tokens), which never falls as n_tokens rises; calls that may run at the same
+ * time need one each.  Only enqueues. */
 int bof4_gemm_linear(const void* packed_dev, uint64_t rows, uint64_t cols, const double* cb_host, const void* table_dev,
                      uint64_t n_outliers, const void* x_dev, uint32_t n_tokens, const bof4_layer* layer, void* ws_dev,
                      size_t ws_bytes, void* stream);
@@ -430,8 +432,8 @@ typedef struct {
     uint64_t ld_dy, ld_pre, ld_mul, ld_dmul, ld_dx;
 } bof4_layer_gradient;
 /* ws_dev: bof4_gemm_linear_backward_workspace_bytes(rows, cols, n_tokens) bytes (256-byte aligned), which never falls as
- * n_tokens rises: dz, partial sums, and the decoded matrix in slabs of up to 256 MiB.  Limits: rows <= 2^18, cols <= 32768 and a
- * multiple of 32, n_tokens <= 65536.  Only enqueues. */
+ * n_tokens rises: dz, partial sums, and the decoded matrix in slabs of up to 256 MiB; calls that may run at the same time need
+ * one each.  Limits: rows <= 2^18, cols <= 32768 and a multiple of 32, n_tokens <= 65536.  Only enqueues. */
 int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t cols, const double* cb_host, const void* table_dev,
                               uint64_t n_outliers, uint32_t n_tokens, const bof4_layer_gradient* gradient, void* ws_dev,
                               size_t ws_bytes, void* stream);
@@ -452,7 +454,8 @@ size_t bof4_gemm_linear_backward_workspace_bytes(uint64_t rows, uint64_t cols, u
  *   top         0 .. 64 alternatives; a row with fewer logits above -inf has -1 and -inf in the places left over
  *   entropy_dev, stats_dev   n_rows and n_rows x 2 values, or NULL.  stats: the row's largest logit m and
  *               log sum_j exp(x_j - m), for bof4_token_logprobs_backward; their sum is the log of the sum of exponentials
- *   ws_dev      bof4_token_logprobs_workspace_bytes(n_rows, vocab, top) bytes (256-byte aligned); contents undefined after
+ *   ws_dev      bof4_token_logprobs_workspace_bytes(n_rows, vocab, top) bytes (256-byte aligned); contents undefined after;
+ *               calls that may run at the same time need one each
  * A row of nothing but -inf: logprob -inf, entropy 0, no alternatives, stats (-inf, 0).  A row that holds a NaN or
  * +inf: every value of it NaN (but the logprob of no target), no alternatives.  Limits: n_rows <= 2^23, vocab <= 2^30.
  * Only enqueues.
@@ -470,7 +473,7 @@ size_t bof4_token_logprobs_workspace_bytes(uint64_t n_rows, uint64_t vocab, uint
  *   target_dev and d_logprob_dev   both, or neither (then g = 0); a target that asks for nothing has g = 0 as well
  *   entropy_dev and d_entropy_dev  both, or neither (then h = 0); entropy as bof4_token_logprobs wrote it
  *   d_logits_dev  n_rows x vocab of d_logits_type, row stride ld_d_logits (>= vocab), all of it written; may be the logits
- *               themselves (one type and one row stride)
+ *               themselves (one type and one row stride), else apart from them
  * A logit of -inf and a row of nothing else have a gradient of 0 (the target's own part g aside); a row with a NaN or +inf
  * has NaN.  Limits as above, and fewer than 2^24 stretches of 2048 logits.  Only enqueues.
  */

@@ -25,8 +25,9 @@ __device__ __forceinline__ float load_logit(const void* p, uint64_t i) {
     else return reinterpret_cast<const float*>(p)[i];
 }
 
-// m, S and T of a part of a row.  u = x - m is kept above -1e30 where it is a factor only, so that a logit without
-// probability (e = 0, u = -inf) adds 0 and not NaN to T.
+// m, S and T of a part of a row.  Where u = x - m is a factor next to its exponential (0 below -104) it is kept above -1e4, so that
+// a logit without probability (u = -inf) or far below the others adds 0 and neither NaN nor an overflow.
+constexpr float LOGPROBS_FAR = -1e4f;
 struct RowSums {
     float m, s, t;
 };
@@ -37,7 +38,7 @@ __device__ __forceinline__ RowSums merge_sums(RowSums a, RowSums b) {
     const float m = fmaxf(a.m, b.m), ms = finite_max(m);
     const float ua = a.m - ms, ub = b.m - ms, fa = logprobs_exp(ua), fb = logprobs_exp(ub);
     return {m, a.s * fa + b.s * fb,
-            fa * fmaf(a.s, fmaxf(ua, -1e30f), a.t) + fb * fmaf(b.s, fmaxf(ub, -1e30f), b.t)};
+            fa * fmaf(a.s, fmaxf(ua, LOGPROBS_FAR), a.t) + fb * fmaf(b.s, fmaxf(ub, LOGPROBS_FAR), b.t)};
 }
 
 // A logit and its id as one number: larger is the larger logit, then the lower id.  0 is less than any.
@@ -330,7 +331,7 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobsArgs a, ui
 #pragma unroll
         for (uint32_t i = 1; i < LOGPROBS_WORDS * PER_WORD; ++i) lane_max = fmaxf(lane_max, x[i]);
         const float m_new = fmaxf(m, lane_max), ms = finite_max(m_new);
-        const float moved = m - ms, f = logprobs_exp(moved), moved_f = fmaxf(moved, -1e30f);
+        const float moved = m - ms, f = logprobs_exp(moved), moved_f = fmaxf(moved, LOGPROBS_FAR);
         t0 = f * fmaf(s0, moved_f, t0);
         t1 = f * fmaf(s1, moved_f, t1);
         s0 *= f;
@@ -341,8 +342,8 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobsArgs a, ui
             const float u0 = x[i] - ms, u1 = x[i + 1] - ms, e0 = logprobs_exp(u0), e1 = logprobs_exp(u1);
             s0 += e0;
             s1 += e1;
-            t0 = fmaf(e0, fmaxf(u0, -1e30f), t0);
-            t1 = fmaf(e1, fmaxf(u1, -1e30f), t1);
+            t0 = fmaf(e0, fmaxf(u0, LOGPROBS_FAR), t0);
+            t1 = fmaf(e1, fmaxf(u1, LOGPROBS_FAR), t1);
         }
         if (a.top > 0) {
             const uint64_t reach = __builtin_amdgcn_ballot_w64(lane_max >= bound);
@@ -479,7 +480,7 @@ __global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobsGradArgs a, 
     const float ms = finite_max(m);
     auto slope = [&](float x) __attribute__((always_inline)) {
         const float lp = (x - ms) - log_s, p = logprobs_exp(lp);
-        return ENTROPY ? -p * fmaf(h, fmaxf(lp, -1e30f) + H, g) : -p * g;
+        return ENTROPY ? -p * fmaf(h, fmaxf(lp, LOGPROBS_FAR) + H, g) : -p * g;
     };
     auto one = [&](uint32_t j) {  // j counted from the first word, as `target`
         const float x = load_logit<BF16>(words, j);

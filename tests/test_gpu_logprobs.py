@@ -361,3 +361,23 @@ def test_results_changed_in_place_leave_what_the_gradient_needs():
     want = keep[:, None].double() * (torch.nn.functional.one_hot(t, 1000) - torch.softmax(x.detach().double(), -1))
     # exp of a difference rounded at 2^-24 of up to 30, and the sum's own error: below 64 half steps of the largest gradient
     assert float((x.grad.double() - want).abs().max()) <= 64 * 2.0 ** -24 * 2
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_large_gradients_of_the_entropy_stay_finite_next_to_logits_without_probability(dtype):
+    """p = 0 there, and with it the gradient, however large d_entropy is."""
+    n, vocab = 5, 3001
+    x, t = make(n, vocab, dtype, 4)
+    x[:, ::3] = -math.inf
+    x[:, 1::7] = -1e30
+    t[:] = 2
+    _, entropy, _, _, stats = binding.bof4_token_logprobs(x, t)
+    g, h = torch.ones(n, device=DEV), torch.tensor([1e9, -1e9, 1e20, 1e30, 1.0], device=DEV)
+    d = binding.bof4_token_logprobs_backward(x, stats, t, g, entropy, h, out_dtype=torch.float32).double()
+    lp = torch.log_softmax(x.double(), -1)
+    p = lp.exp()
+    slope = p * (torch.where(p > 0, lp, 0.0) + entropy.double()[:, None])
+    want = g[:, None] * (torch.nn.functional.one_hot(t, vocab) - p) - h.double()[:, None] * slope
+    # lp, of up to 32, and H are off by some 2^-24 of 32 each, twice over in p: 2^-17 of what is summed up, generously
+    size = g[:, None] + h.double().abs()[:, None] * p * (torch.where(p > 0, lp.abs(), 0.0) + entropy.double()[:, None])
+    assert bool(((d - want).abs() <= 2.0 ** -17 * size).all())
