@@ -547,3 +547,47 @@ def test_gemm_linear_decoded_first_for_results_in_bfloat16(rows, cols, n_tokens,
     check(m, "gemm", n_tokens, "none")
     check(m, "gemm", n_tokens, "silu", mul=f32, pre=bf16)
     check(m, "gemm", n_tokens, "relu", bias=bf16, mul=bf16, residual=f32)
+
+
+@pytest.mark.parametrize("way,rows,cols,n_tokens", [("gemv", 40, 96, 5), ("gemm", 40, 96, 40), ("gemm", 300, 2304, 330), ("gemm", 521, 512, 600)])
+def test_row_strides_past_32_bits(way, rows, cols, n_tokens):
+    """Tokens 2^32 / (n_tokens - 1) elements and more apart, forward and back, against the same call on compact tensors."""
+    m = Matrix(rows, cols, 0.01)
+    stride = ((1 << 32) // (n_tokens - 1) + 8 * rows + 64) // 64 * 64
+    whole = torch.empty(n_tokens * stride, dtype=torch.bfloat16, device=DEV)
+
+    def far(at, values=None):
+        t = whole.as_strided((n_tokens, rows), (stride, 1), at * (rows + 3))
+        return t if values is None else t.copy_(values)
+
+    x, mul, residual = randn((n_tokens, cols), 1), randn((n_tokens, rows), 2), randn((n_tokens, rows), 3)
+    pre = torch.empty((n_tokens, rows), dtype=torch.bfloat16, device=DEV)
+    want = m.linear(way, x, act="silu", mul=mul, residual=residual, pre=pre)
+    y, z = far(0), far(1)
+    m.linear(way, x, act="silu", mul=far(2, mul), residual=far(3, residual), pre=z, out=y)
+    assert torch.equal(y, want) and torch.equal(z, pre)
+    if way == "gemm":
+        dy, dmul = randn((n_tokens, rows), 4), torch.empty((n_tokens, rows), dtype=torch.bfloat16, device=DEV)
+        dbias, dbias_far = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+        dx = m.backward(dy, act="silu", pre=pre, mul=mul, dmul=dmul, dbias=dbias)
+        d = far(4)
+        dx_far = m.backward(far(5, dy), act="silu", pre=z, mul=far(2), dmul=d, dbias=dbias_far)
+        assert torch.equal(dx_far, dx) and torch.equal(d, dmul) and torch.equal(dbias_far, dbias)
+
+
+def test_most_tokens_and_columns():
+    """65536 tokens of 32768 columns: x and its operands are 4 GB each.  The last tokens against binary64, forward and back."""
+    m, n = Matrix(64, 32768, 0.001), 65536
+    x = torch.empty((n, m.cols), dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    for t in range(0, n, 4096):
+        x[t:t + 4096] = torch.randn((4096, m.cols), generator=g, device=DEV, dtype=torch.bfloat16)
+    y = m.linear("gemm", x)
+    picked = torch.tensor([0, 1, 32767, 32768, 49151, 65503, 65504, 65535], device=DEV)
+    x64, w = x[picked].double(), m.gemm_w
+    want, size = x64 @ w.t().contiguous(), x64.abs() @ w.abs().t().contiguous()
+    assert bool(((y[picked].double() - want).abs() <= (m.cols + 64) * U * size + 1.01 * half_step(want, torch.bfloat16)).all())
+    dx = m.backward(y, out=x)  # (over x, which is done with)
+    d64 = y[picked].double()
+    want, size = d64 @ w, d64.abs() @ w.abs()
+    assert bool(((dx[picked].double() - want).abs() <= (m.rows + 64) * U * size + 1.01 * half_step(want, torch.bfloat16)).all())
