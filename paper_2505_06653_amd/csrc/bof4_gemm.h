@@ -778,7 +778,9 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_wide_kernel(
 // One wave per GEMM_DECODE_TILES tiles of one row tile, all of whose codes are on their way at once; the first launch of a call
 // reorders x as well (pack_groups workgroups, gemm_pack_x).  Bound by memory: 50 M
 // weights in 23 us (5.7 TB/s) where what it writes stays in the 256 MB cache behind the L2s, half of that beyond.
-constexpr uint32_t GEMM_DECODE_TILES = 4, GEMM_DECODE_WAVES = 4;
+// Two tiles a wave against four and one: products whole, 64 shapes of 640 to 4000 tokens with and without a list, 0.994 of the time of
+// four in the mean (0.96 to 1.015); one 0.994 (0.95 to 1.034).
+constexpr uint32_t GEMM_DECODE_TILES = 2, GEMM_DECODE_WAVES = 4;
 template <bool OUTLIERS>
 __global__ __launch_bounds__(64 * GEMM_DECODE_WAVES) void gemm_decode_kernel(
     const char* __restrict__ packed, uint32_t first_rt, uint32_t n_rt, uint32_t n_chunks, CodebookArgs cb,
