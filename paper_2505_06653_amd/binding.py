@@ -695,14 +695,14 @@ def _table(table, rows, cols, n_outliers, gpu):
     if table is None:
         raise ValueError("outliers need their table (bof4_gemv_outlier_table, bof4_gemm_outlier_table)")
     # (bof4_gemv_outlier_table_bytes)
-    if table.get_device() != gpu or table.numel() < (((rows * -(-cols // 2048) + 1) * 4 + 7) & ~7) + 8 * k:
-        raise ValueError("the outlier table must be on the current GPU and have bof4_gemv_outlier_table_bytes(rows, cols, n_outliers) bytes")
+    if table.get_device() != gpu or not table.is_contiguous() or table.numel() < (((rows * -(-cols // 2048) + 1) * 4 + 7) & ~7) + 8 * k:
+        raise ValueError("the outlier table must be on the current GPU, contiguous, of bof4_gemv_outlier_table_bytes(rows, cols, n_outliers) bytes")
     return table.data_ptr(), k
 
 
 def _packed(packed, rows, cols, gpu):
-    if packed.get_device() != gpu or packed.numel() < bof4_gemm_packed_bytes(rows, cols):
-        raise ValueError("the packed matrix must be on the current GPU and not too small for rows x cols (bof4_gemm_pack)")
+    if packed.get_device() != gpu or not packed.is_contiguous() or packed.numel() < bof4_gemm_packed_bytes(rows, cols):
+        raise ValueError("the packed matrix must be on the current GPU, contiguous and not too small for rows x cols (bof4_gemm_pack)")
     return packed.data_ptr()
 
 
@@ -733,8 +733,9 @@ def bof4_gemv_linear(codes, scales, rows, cols, block, cb, x, table=None, n_outl
     x2 = _layer_input(x, cols, gpu)
     n_tokens = x2.shape[0]
     table_at, k = _table(table, rows, cols, n_outliers, gpu)
-    if codes.get_device() != gpu or scales.get_device() != gpu or 2 * codes.numel() < rows * cols or scales.numel() * block < rows * cols:
-        raise ValueError("codes and scales must be on the current GPU and have those of rows x cols weights")
+    if codes.get_device() != gpu or scales.get_device() != gpu or 2 * codes.numel() < rows * cols or scales.numel() * block < rows * cols \
+            or not codes.is_contiguous() or not scales.is_contiguous() or scales.element_size() != 2:
+        raise ValueError("codes and scales (2 bytes each) must be on the current GPU, contiguous, and those of rows x cols weights")
     if out is None:
         out = torch.empty((n_tokens, rows), dtype=out_dtype, device=x.device)
     layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out, gpu)

@@ -591,3 +591,25 @@ def test_most_tokens_and_columns():
     d64 = y[picked].double()
     want, size = d64 @ w, d64.abs() @ w.abs()
     assert bool(((dx[picked].double() - want).abs() <= (m.rows + 64) * U * size + 1.01 * half_step(want, torch.bfloat16)).all())
+
+
+def test_refusals_of_views_that_hold_fewer_numbers_than_they_show():
+    m = Matrix(64, 96, 0.05)
+    x, r = randn((3, 96), 1), randn((3, 64), 2)
+    wide = [torch.zeros(1, dtype=t.dtype, device=DEV).expand(2 * t.numel()) for t in (m.codes, m.scales, m.packed, m.gemm_table)]
+    codes, scales, packed, table = wide
+    for call in (lambda: binding.bof4_gemv_linear(codes, m.scales, 64, 96, 32, m.cb, x), lambda: binding.bof4_gemv_linear(m.codes, scales, 64, 96, 32, m.cb, x),
+                 lambda: binding.bof4_gemv_linear(m.codes, m.scales.float(), 64, 96, 32, m.cb, x),
+                 lambda: binding.bof4_gemv_linear(m.codes, m.scales, 64, 96, 32, m.cb, x, table, m.k),
+                 lambda: binding.bof4_gemm_linear(packed, 64, 96, m.cb, x), lambda: binding.bof4_gemm_linear(m.packed, 64, 96, m.cb, x, table, m.k),
+                 lambda: binding.bof4_gemm_linear_backward(packed, 64, 96, m.cb, r),
+                 lambda: binding.bof4_gemm_linear(m.packed, 64, 96, m.cb, x, residual=r[:1].expand(3, 64).t().t()[:, :63])):
+        with pytest.raises(ValueError):
+            call()
+    for kw in (dict(residual=r[:1].expand(3, 64)), dict(mul=r[:1].expand(3, 64)), dict(out=r[:1].expand(3, 64))):
+        with pytest.raises(binding.Bof4Error):  # rows on top of each other
+            binding.bof4_gemm_linear(m.packed, 64, 96, m.cb, x, **kw)
+    with pytest.raises(binding.Bof4Error):
+        binding.bof4_gemm_linear_backward(m.packed, 64, 96, m.cb, r[:1].expand(3, 64))
+    with pytest.raises(binding.Bof4Error):
+        binding.bof4_token_logprobs(torch.zeros((1, 9), device=DEV).expand(3, 9))
