@@ -180,8 +180,7 @@ struct GemmDecodedPlan {
 };
 // `layer`: by the time of the tile that gemm_decoded_tile picks.  (A plain product's splits and slabs stay as the 256 x 128 tile
 // wants them, and with them the order of its additions.)
-inline GemmDecodedPlan gemm_decoded_plan(uint64_t rows, uint64_t cols, uint64_t tok_tiles, bool layer = false) {
-    const uint64_t tok_groups = (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES;
+inline GemmDecodedPlan gemm_decoded_group_plan(uint64_t rows, uint64_t cols, uint64_t tok_groups, bool layer) {
     const uint64_t groups = (rows + GEMM_WIDE_WAVES * GEMM_ROWS - 1) / (GEMM_WIDE_WAVES * GEMM_ROWS);
     const uint64_t chunks = (cols + GEMM_CHUNK - 1) / GEMM_CHUNK, slots = tok_groups * GEMM_WIDE_TOK_TILES * GEMM_TOKENS;
     const uint64_t group_bytes = chunks * GEMM_WIDE_WAVES * GEMM_TILE_WORDS * 16, most = GEMM_DECODED_BYTES / group_bytes;
@@ -204,14 +203,25 @@ inline GemmDecodedPlan gemm_decoded_plan(uint64_t rows, uint64_t cols, uint64_t 
                 best = {(uint32_t)(slab * GEMM_WIDE_WAVES), (uint32_t)split, (uint32_t)per, time, (size_t)(slab * group_bytes), 0, false};
         }
     }
-    best.time += 6.0 + 0.8e-6 * (double)(tok_tiles * GEMM_TOKENS * cols);
     return best;
+}
+inline double gemm_decoded_x_time(uint64_t cols, uint64_t tok_tiles) {  // and what the call takes besides
+    return 6.0 + 0.8e-6 * (double)(tok_tiles * GEMM_TOKENS * cols);
+}
+inline GemmDecodedPlan gemm_decoded_plan(uint64_t rows, uint64_t cols, uint64_t tok_tiles) {
+    GemmDecodedPlan D = gemm_decoded_group_plan(rows, cols, (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES, false);
+    D.time += gemm_decoded_x_time(cols, tok_tiles);
+    return D;
+}
+inline bool gemm_decodable(uint64_t rows, uint64_t cols, uint64_t tok_groups) {
+    const uint64_t wg_rows = GEMM_WIDE_WAVES * GEMM_ROWS;
+    return tok_groups >= 2 && cols >= 512 && cols <= GEMM_MAX_COLS && (rows + wg_rows - 1) / wg_rows * tok_groups < (1ull << 23);
 }
 // The plan where the product is decoded first, else slab_tiles = 0.  W: gemm_wide_choice's answer.
 inline GemmDecodedPlan gemm_decoded_choice(uint64_t rows, uint64_t cols, uint64_t tok_tiles, bool list, const GemmWideSplit& W) {
     const GemmDecodedPlan no = {0, 0, 0, 0.0, 0, 0, false};
     const uint64_t wg_rows = GEMM_WIDE_WAVES * GEMM_ROWS, tok_groups = (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES;
-    if (tok_groups < 2 || cols < 512 || cols > GEMM_MAX_COLS || (rows + wg_rows - 1) / wg_rows * tok_groups >= (1ull << 23)) return no;
+    if (!gemm_decodable(rows, cols, tok_groups)) return no;
     // (what carrying costs: 21 % of the wide kernel's time where a chain is four chunks, 11 % at eight)
     const GemmChains C = gemm_chains(rows, cols, tok_tiles * GEMM_TOKENS, list);
     const double flush = (double)C.wide_flush;
@@ -246,20 +256,23 @@ inline GemmDecodedPlan gemm_decoded_choice(uint64_t rows, uint64_t cols, uint64_
     return (kind ? 1.03 : 0.98) * D.time * cost + 1.0 < other ? D : no;
 }
 
+inline GemmDecodedPlan gemm_decoded_group_plan_bf16(uint64_t rows, uint64_t cols, uint64_t tok_tiles) {
+    const uint64_t tok_groups = (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES;
+    if (!gemm_decodable(rows, cols, tok_groups)) return {0, 0, 0, 0.0, 0, 0, false};
+    return gemm_decoded_group_plan(rows, cols, tok_groups, true);
+}
 // The same for a layer whose results are all rounded to bfloat16: decoded first wherever that is faster (gemm_plan says why the
 // chains of additions need no care there).  The models put decoding first 3 to 30 % too high on layers, and the other kernels 10 %
 // too low with a list.  Other kernel / decoded first, us: 11008 x 4096 with 300 tokens 88 / 69, 22016 x 4096 with 500 175 / 146 and
 // with a list and 300 177 / 137, 8192 x 8192 with 300 98 / 92, but 4096 x 11008 with 300 59 / 69 and 4096 x 4096 with 256 37 / 39.
 // Over 172 layers of 1000 to 28672 rows, 1024 to 16640 columns and 130 to 4000 tokens this choice is 0.95 to 1.24 times as fast
 // as gemm_decoded_choice's, 1.2 % faster in the mean; over 180 of 64 to 2500 rows and 512 to 2560 columns 0.92 to 1.47, 10 %.
-inline GemmDecodedPlan gemm_decoded_choice_bf16(uint64_t rows, uint64_t cols, uint64_t tok_tiles, bool list, const GemmWideSplit& W) {
-    const GemmDecodedPlan no = {0, 0, 0, 0.0, 0, 0, false};
-    const uint64_t wg_rows = GEMM_WIDE_WAVES * GEMM_ROWS, tok_groups = (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES;
-    if (tok_groups < 2 || cols < 512 || cols > GEMM_MAX_COLS || (rows + wg_rows - 1) / wg_rows * tok_groups >= (1ull << 23)) return no;
+// G: gemm_decoded_group_plan_bf16's answer, which is the same for all token tiles of a group.
+inline GemmDecodedPlan gemm_decoded_choice_bf16(uint64_t rows, uint64_t cols, uint64_t tok_tiles, bool list, const GemmWideSplit& W,
+                                                GemmDecodedPlan G) {
     const double other = (list ? 1.1 : 1.0) * (W.split > 0 ? W.time : gemm_kernel_time(rows, cols, tok_tiles));
-    if (0.95 * (10.0 + 0.46e-6 * (double)(rows * cols)) >= other) return no;  // (no plan is shorter)
-    const GemmDecodedPlan D = gemm_decoded_plan(rows, cols, tok_tiles, true);
-    return 0.95 * D.time < other ? D : no;
+    if (G.slab_tiles > 0 && 0.95 * (G.time + gemm_decoded_x_time(cols, tok_tiles)) >= other) G.slab_tiles = 0;
+    return G;
 }
 
 // Workspace of bof4_gemm: x in the order of the products, then the partial results of the workgroups that share a row.
@@ -294,15 +307,16 @@ inline GemmWsLayout gemm_ws_layout(uint64_t rows, uint64_t cols, uint64_t n_toke
 // tokens).  Splits and slabs are the same for all token tiles of a group, so the most tokens of a group for which a kernel is
 // chosen need the most: 8192 x 28672 at 2000 / 65536 tokens 29 us / 0.37 ms, 4096 x 4096 15 us / 0.18 ms (45 / 1500 and 30 / 1000
 // where every token tile is asked about).
-// A layer's covers both types of results.
+// A layer's covers both types of results, in half as much time again.
 inline size_t gemm_ws_bytes(uint64_t rows, uint64_t cols, uint64_t n_tokens, bool layer = false) {
     size_t need = gemm_ws_layout(rows, cols, n_tokens).total;
     const uint64_t most = n_tokens < GEMM_MAX_TOKENS ? n_tokens : GEMM_MAX_TOKENS;
     const uint64_t all_tiles = (most + GEMM_TOKENS - 1) / GEMM_TOKENS;
     for (uint64_t below = 0; below < all_tiles; below += GEMM_WIDE_TOK_TILES) {  // the token tiles before a group
         bool has_wide = false, has_decoded = false, has_bf16 = !layer;
-        for (uint64_t tiles = below + GEMM_WIDE_TOK_TILES < all_tiles ? below + GEMM_WIDE_TOK_TILES : all_tiles;
-             tiles > below && !(has_wide && has_decoded && has_bf16); --tiles) {
+        const uint64_t last = below + GEMM_WIDE_TOK_TILES < all_tiles ? below + GEMM_WIDE_TOK_TILES : all_tiles;
+        const GemmDecodedPlan G = layer ? gemm_decoded_group_plan_bf16(rows, cols, last) : GemmDecodedPlan{};
+        for (uint64_t tiles = last; tiles > below && !(has_wide && has_decoded && has_bf16); --tiles) {
             const uint64_t t = tiles * GEMM_TOKENS < most ? tiles * GEMM_TOKENS : most;  // the most tokens in them
             for (const bool list : {true, false}) {  // (which kernel is chosen depends on it, neither way the other's superset)
                 const GemmWideSplit W = gemm_wide_choice(rows, cols, tiles, list);
@@ -314,7 +328,7 @@ inline size_t gemm_ws_bytes(uint64_t rows, uint64_t cols, uint64_t n_tokens, boo
                 for (const bool bf16 : {false, true}) {
                     bool& has = bf16 ? has_bf16 : has_decoded;
                     if (has) continue;
-                    const GemmDecodedPlan D = bf16 ? gemm_decoded_choice_bf16(rows, cols, tiles, list, W)
+                    const GemmDecodedPlan D = bf16 ? gemm_decoded_choice_bf16(rows, cols, tiles, list, W, G)
                                                    : gemm_decoded_choice(rows, cols, tiles, list, W);
                     if (D.slab_tiles == 0) continue;
                     const size_t bytes = gemm_ws_layout(rows, cols, t).decoded(D.split, t, rows, layer) + D.slab_bytes;
@@ -348,7 +362,7 @@ inline GemmPlan gemm_plan(uint64_t rows, uint64_t cols, uint64_t n_tokens, bool 
     GemmPlan P;
     P.ws = gemm_ws_layout(rows, cols, n_tokens);
     P.wide = gemm_wide_choice(rows, cols, tok_tiles, list);
-    P.decoded = bf16 ? gemm_decoded_choice_bf16(rows, cols, tok_tiles, list, P.wide)
+    P.decoded = bf16 ? gemm_decoded_choice_bf16(rows, cols, tok_tiles, list, P.wide, gemm_decoded_group_plan_bf16(rows, cols, tok_tiles))
                      : gemm_decoded_choice(rows, cols, tok_tiles, list, P.wide);
     P.chains = gemm_chains(rows, cols, n_tokens, list);
     if (bf16) {
