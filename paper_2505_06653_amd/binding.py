@@ -660,10 +660,10 @@ def _flat(t, name, dtypes, shape, dev):
 _F32, _I64, _U8 = (torch.float32,), (torch.int64,), (torch.uint8,)
 
 
-def _scratch(ws, nbytes, device, stream):
+def _scratch(ws, nbytes, device, stream, gpu):
     """The caller's workspace, or one of `nbytes` that the allocator keeps until `stream` is done with it."""
     if ws is not None:
-        _flat(ws, "ws", _U8, None, torch.cuda.current_device())
+        _flat(ws, "ws", _U8, None, gpu)
         return ws
     ws = torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
     if stream is not None:
@@ -761,7 +761,7 @@ def bof4_gemm_linear(packed, rows, cols, cb, x, table=None, n_outliers=0, bias=N
     if out is None:
         out = torch.empty((n_tokens, rows), dtype=out_dtype, device=x.device)
     layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out, gpu)
-    ws = _scratch(ws, 0 if ws is not None else bof4_gemm_linear_workspace_bytes(rows, cols, n_tokens), x.device, stream)
+    ws = _scratch(ws, 0 if ws is not None else bof4_gemm_linear_workspace_bytes(rows, cols, n_tokens), x.device, stream, gpu)
     _check(lib().bof4_gemm_linear(packed_at, rows, cols, cbp, table_at, k, x2.data_ptr(), n_tokens, layer, ws.data_ptr(),
                                   ws.numel(), _stream(stream)))
     return out
@@ -797,7 +797,7 @@ def bof4_gemm_linear_backward(packed, rows, cols, cb, dy, table=None, n_outliers
         dbias_at = _flat(dbias, "dbias", _F32, (rows,), gpu)
     g = LAYER_GRADIENT.pack(_activation(act), _TYPES[dy.dtype], pre_type, mul_type, dmul_type, _TYPES[out.dtype], dy_at, pre_at,
                             mul_at, dmul_at, dbias_at, dx_at, _row_stride(dy), ld_pre, ld_mul, ld_dmul, _row_stride(out))
-    ws = _scratch(ws, 0 if ws is not None else bof4_gemm_linear_backward_workspace_bytes(rows, cols, n_tokens), dy.device, stream)
+    ws = _scratch(ws, 0 if ws is not None else bof4_gemm_linear_backward_workspace_bytes(rows, cols, n_tokens), dy.device, stream, gpu)
     _check(lib().bof4_gemm_linear_backward(packed_at, rows, cols, cbp, table_at, k, n_tokens, g, ws.data_ptr(), ws.numel(),
                                            _stream(stream)))
     return out
@@ -822,12 +822,12 @@ def bof4_token_logprobs(logits, targets=None, top=0, ws=None, stream=None):
     logprob = top_idx = top_logprob = targets_at = logprob_at = idx_at = top_at = None
     stats, entropy = new((n, 2), dtype=f32), new(n, dtype=f32)
     if targets is not None:
-        targets_at, logprob = _flat(targets, "targets", _I64, (n,), gpu), new(n, dtype=f32)
+        targets_at, logprob = _flat(targets, "targets", _I64, (n,), gpu), torch.empty_like(entropy)
         logprob_at = logprob.data_ptr()
     if top > 0:
         top_idx, top_logprob = new((n, top), dtype=torch.int64), new((n, top), dtype=f32)
         idx_at, top_at = top_idx.data_ptr(), top_logprob.data_ptr()
-    ws = _scratch(ws, 0 if ws is not None else bof4_token_logprobs_workspace_bytes(n, vocab, top), logits.device, stream)
+    ws = _scratch(ws, 0 if ws is not None else bof4_token_logprobs_workspace_bytes(n, vocab, top), logits.device, stream, gpu)
     _check(lib().bof4_token_logprobs(logits_at, _TYPES[logits.dtype], n, vocab, _row_stride(logits), targets_at, top,
                                      logprob_at, entropy.data_ptr(), idx_at, top_at, stats.data_ptr(), ws.data_ptr(),
                                      ws.numel(), _stream(stream)))
