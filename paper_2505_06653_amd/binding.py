@@ -775,7 +775,8 @@ def bof4_gemm_linear_backward(packed, rows, cols, cb, dy, table=None, n_outliers
                               dbias=None, out=None, out_dtype=torch.bfloat16, ws=None, stream=None):
     """The gradients of bof4_gemm_linear: returns dx [n_tokens, cols] (`out`, else of `out_dtype`) from dy [n_tokens, rows] and,
     as the forward call had them, act, pre (what it wrote) and mul.  `dmul` [n_tokens, rows] and `dbias` float32 [rows]: tensors
-    that receive those gradients (the residual's is dy)."""
+    that receive those gradients (the residual's is dy).  dy * mul * act'(pre) enters the product rounded to bfloat16 if dy and dx
+    are bfloat16, in sixteen bits if dy is float32, whole if dx is float32 (two and three times the products)."""
     cb, cbp = _cb(cb)
     if dy.dim() != 2 or dy.shape[1] != rows:
         raise ValueError("dy must be [n_tokens, rows]")

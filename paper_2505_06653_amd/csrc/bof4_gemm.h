@@ -902,7 +902,8 @@ __device__ __forceinline__ void gemm_bare_barrier() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
-template <bool CARRY, int ROW_TILES, class Out>
+//   TERMS: x is there in that many bfloat16 terms, one tile per chunk and term; n_chunks and per_split count them all.
+template <bool CARRY, int ROW_TILES, uint32_t TERMS, class Out>
 __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
     const uint4* __restrict__ decoded, uint32_t first_row, uint32_t n_rt, uint32_t rows, uint32_t n_chunks,
     const uint4* __restrict__ xp, uint32_t tok_tiles, uint32_t tok_groups, uint32_t per_split, uint32_t flush,
@@ -933,18 +934,20 @@ __global__ __launch_bounds__(64 * GEMM_WIDE_WAVES, 2) void gemm_decoded_kernel(
 #pragma unroll
     for (int i = 0; i < REQUESTS; ++i) {
         const uint32_t tile = (wave * REQUESTS + i) / 4, j = (wave * REQUESTS + i) % 4;
-        const uint4* tiles = tile < ROW_TILES ? decoded + (uint64_t)min(rg * ROW_TILES + tile, n_rt - 1) * n_chunks * GEMM_TILE_WORDS
+        const uint4* tiles = tile < ROW_TILES ? decoded + (uint64_t)min(rg * ROW_TILES + tile, n_rt - 1) * (n_chunks / TERMS) * GEMM_TILE_WORDS
                                               : xp + (uint64_t)min(tg * GEMM_WIDE_TOK_TILES + tile - ROW_TILES, tok_tiles - 1) * n_chunks * GEMM_TILE_WORDS;
         from[i] = tiles + 64 * j + lane;
     }
     // Past the last chunk the last one is asked for again, so that there are always as many requests.
     auto bring = [&](uint32_t nth, uint32_t buf) __attribute__((always_inline)) {
-        const uint64_t at = (uint64_t)min(ch0 + nth, ch1 - 1) * GEMM_TILE_WORDS;
+        const uint32_t chunk = min(ch0 + nth, ch1 - 1);
+        const uint64_t at = (uint64_t)chunk * GEMM_TILE_WORDS, at_row = (uint64_t)(chunk / TERMS) * GEMM_TILE_WORDS;
         typedef const __attribute__((address_space(1))) void* G;
         typedef __attribute__((address_space(3))) void* L;
 #pragma unroll
         for (int i = 0; i < REQUESTS; ++i)
-            __builtin_amdgcn_global_load_lds((G)(from[i] + at), (L)&sh[buf][0][(wave * REQUESTS + i) * 64], 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((G)(from[i] + ((wave * REQUESTS + i) / 4 < ROW_TILES ? at_row : at)),
+                                             (L)&sh[buf][0][(wave * REQUESTS + i) * 64], 16, 0, 0);
     };
     gemm_f32x16 acc[RW][TW], sum[RW][TW];  // [row tile][token tile]
 #pragma unroll

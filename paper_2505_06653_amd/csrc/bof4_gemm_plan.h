@@ -179,11 +179,13 @@ struct GemmDecodedPlan {
     bool carry;
 };
 // `layer`: by the time of the tile that gemm_decoded_tile picks.  (A plain product's splits and slabs stay as the 256 x 128 tile
-// wants them, and with them the order of its additions.)
-inline GemmDecodedPlan gemm_decoded_group_plan(uint64_t rows, uint64_t cols, uint64_t tok_groups, bool layer) {
+// wants them, and with them the order of its additions.)  `terms`: bfloat16 terms of the other operand that a chunk is multiplied
+// with; split and per_split count a chunk once for each.
+inline GemmDecodedPlan gemm_decoded_group_plan(uint64_t rows, uint64_t cols, uint64_t tok_groups, bool layer, uint64_t terms = 1) {
     const uint64_t groups = (rows + GEMM_WIDE_WAVES * GEMM_ROWS - 1) / (GEMM_WIDE_WAVES * GEMM_ROWS);
-    const uint64_t chunks = (cols + GEMM_CHUNK - 1) / GEMM_CHUNK, slots = tok_groups * GEMM_WIDE_TOK_TILES * GEMM_TOKENS;
-    const uint64_t group_bytes = chunks * GEMM_WIDE_WAVES * GEMM_TILE_WORDS * 16, most = GEMM_DECODED_BYTES / group_bytes;
+    const uint64_t matrix_chunks = (cols + GEMM_CHUNK - 1) / GEMM_CHUNK, chunks = terms * matrix_chunks;
+    const uint64_t slots = tok_groups * GEMM_WIDE_TOK_TILES * GEMM_TOKENS;
+    const uint64_t group_bytes = matrix_chunks * GEMM_WIDE_WAVES * GEMM_TILE_WORDS * 16, most = GEMM_DECODED_BYTES / group_bytes;
     const uint64_t least_slabs = (groups + most - 1) / most;
     GemmDecodedPlan best = {0, 0, 0, 0.0, 0, 0, false};
     for (uint64_t n_slabs = least_slabs; n_slabs <= least_slabs + 2 && n_slabs <= groups; ++n_slabs) {
@@ -208,8 +210,8 @@ inline GemmDecodedPlan gemm_decoded_group_plan(uint64_t rows, uint64_t cols, uin
 inline double gemm_decoded_x_time(uint64_t cols, uint64_t tok_tiles) {  // and what the call takes besides
     return 6.0 + 0.8e-6 * (double)(tok_tiles * GEMM_TOKENS * cols);
 }
-inline GemmDecodedPlan gemm_decoded_plan(uint64_t rows, uint64_t cols, uint64_t tok_tiles) {
-    GemmDecodedPlan D = gemm_decoded_group_plan(rows, cols, (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES, false);
+inline GemmDecodedPlan gemm_decoded_plan(uint64_t rows, uint64_t cols, uint64_t tok_tiles, uint64_t terms = 1) {
+    GemmDecodedPlan D = gemm_decoded_group_plan(rows, cols, (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES, false, terms);
     D.time += gemm_decoded_x_time(cols, tok_tiles);
     return D;
 }

@@ -4,10 +4,13 @@
 //
 // dx contracts over the rows of W^, so the matrix cores want it turned.  A call works in two steps, as the product for many
 // tokens does whose matrix is decoded first: linear_turn_kernel decodes the packed matrix into the operands of W^^T, in
-// slabs that stay in the cache behind the L2s, and gemm_decoded_kernel multiplies them with dz.  dz is rounded to bfloat16
-// once, which is what the matrix cores take: each term is off by 2^-8 of itself at most, as far as dx's own rounding to
-// bfloat16 (without activation and factor dz is dy, and nothing is rounded).  linear_dz makes it from dy in the
+// slabs that stay in the cache behind the L2s, and gemm_decoded_kernel multiplies them with dz.  linear_dz makes dz from dy in the
 // order of the operands, and dmul and dbias on the way.
+//   The matrix cores take bfloat16, so dz is the sum of one to three bfloat16 terms, each multiplied with the same decoded
+// chunk (linear_dz_terms).  dy and dx in bfloat16: one, off by 2^-8 of dz at most, as far as dx's own rounding.
+// (dx is then off by 0.0024 of its size where the rounding of the result alone makes 0.0017; a second term would leave just that,
+// at 49 us instead of 38 for 4096 x 4096 with 333 tokens and 398 instead of 230 for 11008 x 4096 with 2000.)  dx in bfloat16 from
+// binary32 dy: two, off by 2^-16.  dx in binary32: three, which hold all 24 bits (59 and 555 us), or as few as hold dz.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -23,11 +26,18 @@ struct LinearGradArgs {
     void* dmul;                  // null: not wanted
     float* dbias_parts;          // null: not wanted
     uint64_t ld_dy, ld_pre, ld_mul, ld_dmul;
-    uint32_t act;
+    uint32_t act, terms;
     bool dy_bf16, pre_bf16, mul_bf16, dmul_bf16;
 };
+constexpr uint32_t LINEAR_MOST_TERMS = 3;
+inline uint32_t linear_dz_terms(uint32_t act, bool dy_bf16, bool mul, bool mul_bf16, bool dx_bf16) {
+    const uint32_t wanted = !dx_bf16 ? 3 : dy_bf16 ? 1 : 2;
+    // without a curved activation dz is dy (or 0), or its product with the factor: eight bits times eight are sixteen
+    const uint32_t exact = act > ACT_RELU || !dy_bf16 || (mul && !mul_bf16) ? 3 : mul ? 2 : 1;
+    return wanted < exact ? wanted : exact;
+}
 
-// dz in the products' order (gemm_pack_x_kernel's, rows in the place of columns): a workgroup takes a chunk of 64 rows and
+// dz in the products' order (gemm_pack_x_kernel's, rows in the place of columns, a chunk's terms behind each other): a workgroup takes a chunk of 64 rows and
 // `tiles_per_range` tiles of 32 tokens, eight threads per token, which read 128 consecutive bytes and write 16-byte words of
 // which eight neighbouring tokens make up 128.  Bound by memory: 2000 tokens x 11008 rows with factor, activation and dmul, 220
 // MB, 44 us (5.0 TB/s; with 8-byte accesses 55).
@@ -42,10 +52,10 @@ __device__ __forceinline__ void linear_dz(uint32_t chunk, uint32_t range, Linear
     const uint32_t tile1 = min(tok_tiles, (range + 1) * tiles_per_range);
     for (uint32_t tile = range * tiles_per_range; tile < tile1; ++tile) {
         const uint64_t t = tile * GEMM_TOKENS + token_in_tile;
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
+        float dy[8] = {};
         if (t < n_tokens && row < rows) {
             const uint32_t n = rows - row;
-            float dy[8], z[8] = {}, f[8], value, slope;
+            float z[8] = {}, f[8], value, slope;
             load_row<8>(a.dy, t * a.ld_dy + row, a.dy_bf16, n, dy);
             if (a.pre) load_row<8>(a.pre, t * a.ld_pre + row, a.pre_bf16, n, z);
             if (a.mul) load_row<8>(a.mul, t * a.ld_mul + row, a.mul_bf16, n, f);
@@ -59,11 +69,20 @@ __device__ __forceinline__ void linear_dz(uint32_t chunk, uint32_t range, Linear
                 bias[i] += dy[i];
             }
             if (a.dmul) store_row<8>(a.dmul, t * a.ld_dmul + row, a.dmul_bf16, n, z);
+        }
+        uint4* to = xp + ((uint64_t)tile * n_chunks + chunk) * a.terms * GEMM_TILE_WORDS + (word & 3) * 64 + (word >> 2) * 32 + token_in_tile;
+        for (uint32_t term = 0;;) {
+            uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = gemm_pack_bf16(dy[2 * i], dy[2 * i + 1]);
+            to[term * GEMM_TILE_WORDS] = make_uint4(w[0], w[1], w[2], w[3]);
+            if (++term == a.terms) break;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {  // what the term leaves; nothing where it is not finite
+                const float rounded = __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+                dy[i] = fabsf(rounded) < INFINITY ? dy[i] - rounded : 0.0f;
+            }
         }
-        xp[((uint64_t)tile * n_chunks + chunk) * GEMM_TILE_WORDS + (word & 3) * 64 + (word >> 2) * 32 + token_in_tile] =
-            make_uint4(w[0], w[1], w[2], w[3]);
     }
     if (!a.dbias_parts) return;
 #pragma unroll

@@ -50,33 +50,35 @@ int layer_out(const bof4_layer* layer, uint64_t rows, const void* x_dev, LayerOu
     return BOF4_OK;
 }
 
-// How the gradient by x is taken: W^^T in slabs of column tiles (the rows of the turned matrix), its rows' chunks over
-// `split` workgroups, and where things lie in the workspace.
+// How the gradient by x is taken: W^^T in slabs of column tiles (the rows of the turned matrix), its rows' chunks, once for each
+// term of dz, over `split` workgroups, and where things lie in the workspace.
 struct LinearBackwardPlan {
     GemmDecodedPlan turned;
     uint32_t ranges, tiles_per_range;  // of the tokens, for dbias
     size_t dbias, parts, decoded, total;
 };
-LinearBackwardPlan backward_plan_one(uint64_t rows, uint64_t cols, uint64_t n_tokens) {
+LinearBackwardPlan backward_plan_one(uint64_t rows, uint64_t cols, uint64_t n_tokens, uint64_t terms) {
     const uint64_t tok_tiles = (n_tokens + GEMM_TOKENS - 1) / GEMM_TOKENS, row_chunks = (rows + GEMM_CHUNK - 1) / GEMM_CHUNK;
     LinearBackwardPlan P;
-    P.turned = gemm_decoded_plan(cols, rows, tok_tiles);
+    P.turned = gemm_decoded_plan(cols, rows, tok_tiles, terms);
     const uint64_t per = (tok_tiles + LINEAR_MOST_RANGES - 1) / LINEAR_MOST_RANGES;
     P.tiles_per_range = (uint32_t)per;
     P.ranges = (uint32_t)((tok_tiles + per - 1) / per);
-    P.dbias = align_up(tok_tiles * GEMM_TOKENS * row_chunks * GEMM_CHUNK * 2, 256);
+    P.dbias = align_up(terms * tok_tiles * GEMM_TOKENS * row_chunks * GEMM_CHUNK * 2, 256);
     P.parts = align_up(P.dbias + P.ranges * rows * 4, 256);
     P.decoded = align_up(P.parts + (P.turned.split > 1 ? P.turned.split * n_tokens * cols * 4 : 0), 256);
     P.total = P.decoded + P.turned.slab_bytes;
     return P;
 }
-// Enough for every number of tokens up to this (the split falls as they rise, so the largest need is not that of the most).
+// Enough for every number of terms and of tokens up to this (the split falls as they rise, so the largest need is not that of the most).
 size_t backward_ws_bytes(uint64_t rows, uint64_t cols, uint64_t n_tokens) {
     constexpr uint64_t GROUP = GEMM_WIDE_TOK_TILES * GEMM_TOKENS;
     size_t need = 0;
     for (uint64_t below = 0; below < n_tokens; below += GROUP) {  // (one plan for all token tiles of a group)
-        const size_t bytes = backward_plan_one(rows, cols, below + GROUP < n_tokens ? below + GROUP : n_tokens).total;
-        if (bytes > need) need = bytes;
+        for (uint64_t terms = 1; terms <= LINEAR_MOST_TERMS; ++terms) {
+            const size_t bytes = backward_plan_one(rows, cols, below + GROUP < n_tokens ? below + GROUP : n_tokens, terms).total;
+            if (bytes > need) need = bytes;
+        }
     }
     return need;
 }
@@ -163,7 +165,8 @@ int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t co
         return fail(BOF4_ERR_ARG, "bof4_gemm_linear_backward: dx, dmul and dbias need memory of their own");
     if (!aligned(packed_dev, 16) || !aligned(table_dev, 8) || !aligned(ws_dev, 256))
         return fail(BOF4_ERR_ARG, "bof4_gemm_linear_backward: misaligned pointer (the packed matrix needs 16 bytes, the table 8, the workspace 256)");
-    const LinearBackwardPlan P = backward_plan_one(rows, cols, n_tokens);
+    const uint32_t terms = linear_dz_terms(l.act, l.dy_type == BOF4_BF16, l.mul_dev != nullptr, l.mul_type == BOF4_BF16, l.dx_type == BOF4_BF16);
+    const LinearBackwardPlan P = backward_plan_one(rows, cols, n_tokens, terms);
     if (ws_bytes < P.total) return fail(BOF4_ERR_WORKSPACE, "bof4_gemm_linear_backward: workspace too small");
     const GemmTableLayout T = gemm_table_layout(rows, cols);
     const uint32_t* offsets_dev = (const uint32_t*)table_dev;
@@ -177,7 +180,7 @@ int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t co
     const uint32_t row_chunks = (uint32_t)((rows + GEMM_CHUNK - 1) / GEMM_CHUNK), chunks = (uint32_t)((cols + GEMM_CHUNK - 1) / GEMM_CHUNK);
     const uint32_t tok_tiles = (n_tokens + GEMM_TOKENS - 1) / GEMM_TOKENS;
     const LinearGradArgs a = {l.dy_dev, l.act != ACT_NONE || l.dmul_dev ? l.pre_dev : nullptr, l.mul_dev, l.dmul_dev,
-                              l.dbias_dev ? dbias_parts : nullptr, l.ld_dy, l.ld_pre, l.ld_mul, l.ld_dmul, l.act,
+                              l.dbias_dev ? dbias_parts : nullptr, l.ld_dy, l.ld_pre, l.ld_mul, l.ld_dmul, l.act, terms,
                               l.dy_type == BOF4_BF16, l.pre_type == BOF4_BF16, l.mul_type == BOF4_BF16, l.dmul_type == BOF4_BF16};
     LayerOut out = {};
     out.y = l.dx_dev;
@@ -209,7 +212,10 @@ int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t co
                        offsets_dev, entries_dev, (uint32_t)n_outliers, T.lg, T.row_tiles, decoded, dz);
         if (n_outliers > 0) { BOF4_LAUNCH_TURN(true) } else { BOF4_LAUNCH_TURN(false) }
 #undef BOF4_LAUNCH_TURN
-        gemm_multiply_decoded(D, FLUSH, false, decoded, ct0 * GEMM_ROWS, n_ct, cols, row_chunks, xp, n_tokens, out, s);
+#define BOF4_MULTIPLY(TERMS_) \
+    gemm_multiply_decoded<TERMS_>(D, FLUSH, false, decoded, ct0 * GEMM_ROWS, n_ct, cols, TERMS_ * row_chunks, xp, n_tokens, out, s);
+        if (terms == 1) { BOF4_MULTIPLY(1) } else if (terms == 2) { BOF4_MULTIPLY(2) } else { BOF4_MULTIPLY(3) }
+#undef BOF4_MULTIPLY
     }
     const uint32_t dbias_groups = l.dbias_dev ? (uint32_t)((rows + 255) / 256) : 0;
     if (D.split > 1) {

@@ -118,18 +118,20 @@ void gemm_add_parts(uint32_t split, uint32_t n_tokens, uint64_t rows, const Out&
     }
 }
 
-// A slab of the decoded matrix times x, with 256 or 192 rows to a workgroup.
-template <class Out>
+// A slab of the decoded matrix times x (in TERMS bfloat16 terms, each with a chunk of its own), with 256 or 192 rows to a workgroup.
+template <uint32_t TERMS = 1, class Out>
 void gemm_multiply_decoded(const GemmDecodedPlan& D, uint32_t flush, bool carry, const uint4* decoded, uint32_t first_row, uint32_t n_rt,
                            uint64_t rows, uint32_t chunks, const uint4* xp, uint32_t n_tokens, const Out& dst, hipStream_t s) {
     const uint32_t tok_tiles = (n_tokens + GEMM_TOKENS - 1) / GEMM_TOKENS;
     const uint32_t tok_groups = (tok_tiles + GEMM_WIDE_TOK_TILES - 1) / GEMM_WIDE_TOK_TILES;
     const uint32_t tiles = gemm_decoded_tile(n_rt, tok_groups * D.split, D.per_split).row_tiles, groups = (n_rt + tiles - 1) / tiles;
 #define BOF4_LAUNCH_DECODED(CARRY_, TILES_)                                                                                  \
-    hipLaunchKernelGGL((gemm_decoded_kernel<CARRY_, TILES_, Out>), dim3(tok_groups * groups * D.split), dim3(64 * GEMM_WIDE_WAVES), \
+    hipLaunchKernelGGL((gemm_decoded_kernel<CARRY_, TILES_, TERMS, Out>), dim3(tok_groups * groups * D.split), dim3(64 * GEMM_WIDE_WAVES), \
                        0, s, decoded, first_row, n_rt, (uint32_t)rows, chunks, xp, tok_tiles, tok_groups, D.per_split, flush,  \
                        n_tokens, D.split, dst);
-    if (tiles == 8) {
+    if constexpr (TERMS > 1) {  // (of gradients, whose sums are not carried)
+        if (tiles == 8) { BOF4_LAUNCH_DECODED(false, 8) } else { BOF4_LAUNCH_DECODED(false, 6) }
+    } else if (tiles == 8) {
         if (carry) { BOF4_LAUNCH_DECODED(true, 8) } else { BOF4_LAUNCH_DECODED(false, 8) }
     } else {
         if (carry) { BOF4_LAUNCH_DECODED(true, 6) } else { BOF4_LAUNCH_DECODED(false, 6) }
