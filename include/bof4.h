@@ -434,7 +434,8 @@ typedef struct {
     uint64_t ld_dy, ld_pre, ld_mul, ld_dmul, ld_dx;
 } bof4_layer_gradient;
 /* ws_dev: bof4_gemm_linear_backward_workspace_bytes(rows, cols, n_tokens) bytes (256-byte aligned), which never falls as
- * n_tokens rises: dz in up to three bfloat16 terms, partial sums, and the decoded matrix in slabs of up to 256 MiB; calls that may
+ * n_tokens rises: dz (in several terms as many tokens of it at a time as 4 GiB hold), partial sums, and the decoded matrix in slabs of up to
+ * 256 MiB; calls that may
  * run at the same time need one each.  Limits: rows <= 2^18, cols <= 32768 and a multiple of 32, n_tokens <= 65536.  Only enqueues. */
 int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t cols, const double* cb_host, const void* table_dev,
                               uint64_t n_outliers, uint32_t n_tokens, const bof4_layer_gradient* gradient, void* ws_dev,

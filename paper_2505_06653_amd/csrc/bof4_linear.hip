@@ -52,21 +52,31 @@ int layer_out(const bof4_layer* layer, uint64_t rows, const void* x_dev, LayerOu
 
 // How the gradient by x is taken: W^^T in slabs of column tiles (the rows of the turned matrix), its rows' chunks, once for each
 // term of dz, over `split` workgroups, and where things lie in the workspace.
+//   Several terms take the tokens in passes of as many groups of them as LINEAR_TERMS_BYTES hold, each with the matrix turned anew,
+// so that a large call needs little more memory than with one term: of 2^18 rows that is 2688 tokens in three terms, for which
+// turning 2^18 x 4096 weights costs a fifteenth of the products.
+constexpr uint64_t LINEAR_TERMS_BYTES = 4ull << 30;
 struct LinearBackwardPlan {
     GemmDecodedPlan turned;
-    uint32_t ranges, tiles_per_range;  // of the tokens, for dbias
+    uint32_t passes, tokens;           // of a pass but the last, which takes the rest
+    uint32_t ranges, tiles_per_range;  // of a pass's tokens, for dbias
     size_t dbias, parts, decoded, total;
 };
 LinearBackwardPlan backward_plan_one(uint64_t rows, uint64_t cols, uint64_t n_tokens, uint64_t terms) {
-    const uint64_t tok_tiles = (n_tokens + GEMM_TOKENS - 1) / GEMM_TOKENS, row_chunks = (rows + GEMM_CHUNK - 1) / GEMM_CHUNK;
+    constexpr uint64_t GROUP = GEMM_WIDE_TOK_TILES * GEMM_TOKENS;
+    const uint64_t row_chunks = (rows + GEMM_CHUNK - 1) / GEMM_CHUNK, token_bytes = terms * row_chunks * GEMM_CHUNK * 2;
     LinearBackwardPlan P;
+    const uint64_t most = terms == 1 ? n_tokens : LINEAR_TERMS_BYTES / token_bytes / GROUP * GROUP;
+    P.tokens = (uint32_t)(n_tokens < most ? n_tokens : most);
+    P.passes = (uint32_t)((n_tokens + P.tokens - 1) / P.tokens);
+    const uint64_t tok_tiles = (P.tokens + GEMM_TOKENS - 1) / GEMM_TOKENS;
     P.turned = gemm_decoded_plan(cols, rows, tok_tiles, terms);
     const uint64_t per = (tok_tiles + LINEAR_MOST_RANGES - 1) / LINEAR_MOST_RANGES;
     P.tiles_per_range = (uint32_t)per;
     P.ranges = (uint32_t)((tok_tiles + per - 1) / per);
-    P.dbias = align_up(terms * tok_tiles * GEMM_TOKENS * row_chunks * GEMM_CHUNK * 2, 256);
-    P.parts = align_up(P.dbias + P.ranges * rows * 4, 256);
-    P.decoded = align_up(P.parts + (P.turned.split > 1 ? P.turned.split * n_tokens * cols * 4 : 0), 256);
+    P.dbias = align_up(tok_tiles * GEMM_TOKENS * token_bytes, 256);
+    P.parts = align_up(P.dbias + (uint64_t)P.passes * P.ranges * rows * 4, 256);
+    P.decoded = align_up(P.parts + (P.turned.split > 1 ? P.turned.split * (uint64_t)P.tokens * cols * 4 : 0), 256);
     P.total = P.decoded + P.turned.slab_bytes;
     return P;
 }
@@ -178,10 +188,9 @@ int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t co
     float* dbias_parts = (float*)(ws + P.dbias);
     uint4* decoded = (uint4*)(ws + P.decoded);
     const uint32_t row_chunks = (uint32_t)((rows + GEMM_CHUNK - 1) / GEMM_CHUNK), chunks = (uint32_t)((cols + GEMM_CHUNK - 1) / GEMM_CHUNK);
-    const uint32_t tok_tiles = (n_tokens + GEMM_TOKENS - 1) / GEMM_TOKENS;
-    const LinearGradArgs a = {l.dy_dev, l.act != ACT_NONE || l.dmul_dev ? l.pre_dev : nullptr, l.mul_dev, l.dmul_dev,
-                              l.dbias_dev ? dbias_parts : nullptr, l.ld_dy, l.ld_pre, l.ld_mul, l.ld_dmul, l.act, terms,
-                              l.dy_type == BOF4_BF16, l.pre_type == BOF4_BF16, l.mul_type == BOF4_BF16, l.dmul_type == BOF4_BF16};
+    LinearGradArgs a = {l.dy_dev, l.act != ACT_NONE || l.dmul_dev ? l.pre_dev : nullptr, l.mul_dev, l.dmul_dev,
+                        l.dbias_dev ? dbias_parts : nullptr, l.ld_dy, l.ld_pre, l.ld_mul, l.ld_dmul, l.act, terms,
+                        l.dy_type == BOF4_BF16, l.pre_type == BOF4_BF16, l.mul_type == BOF4_BF16, l.dmul_type == BOF4_BF16};
     LayerOut out = {};
     out.y = l.dx_dev;
     out.ld_y = l.ld_dx;
@@ -198,32 +207,46 @@ int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t co
     // 4096 with 333 / 1000 / 2000 39.9 / 38.5, 64.2 / 63.0, 100.2 / 101.2, 11008 x 4096 with 256 / 512 / 1000 / 2000 67.0 / 61.6, 89.5 /
     // 87.4, 137.0 / 138.0, 230 / 244).
     const bool dz_apart = (uint64_t)n_tokens * rows > (6ull << 20);
-    if (dz_apart)
-        hipLaunchKernelGGL(linear_dz_kernel, dim3(row_chunks, P.ranges), dim3(256), 0, s, a, n_tokens, (uint32_t)rows, row_chunks,
-                           tok_tiles, P.tiles_per_range, xp);
-    for (uint32_t ct0 = 0; ct0 < col_tiles; ct0 += D.slab_tiles) {
-        const uint32_t n_ct = col_tiles - ct0 < D.slab_tiles ? col_tiles - ct0 : D.slab_tiles;
-        const uint64_t jobs = (uint64_t)((n_ct + 1) / 2) * row_chunks;
-        const LinearDzCall dz = {a, ct0 == 0 && !dz_apart ? row_chunks * P.ranges : 0, n_tokens, (uint32_t)rows, tok_tiles, P.tiles_per_range, xp};
+    const uint32_t dbias_groups = l.dbias_dev ? (uint32_t)((rows + 255) / 256) : 0;
+    uint32_t n_parts = 0;  // of dbias
+    for (uint32_t pass = 0; pass < P.passes; ++pass) {
+        const bool last = pass + 1 == P.passes;
+        const uint32_t n = last ? n_tokens - pass * P.tokens : P.tokens, tok_tiles = (n + GEMM_TOKENS - 1) / GEMM_TOKENS;
+        const uint32_t ranges = (tok_tiles + P.tiles_per_range - 1) / P.tiles_per_range;
+        n_parts += ranges;
+        if (dz_apart)
+            hipLaunchKernelGGL(linear_dz_kernel, dim3(row_chunks, ranges), dim3(256), 0, s, a, n, (uint32_t)rows, row_chunks,
+                               tok_tiles, P.tiles_per_range, xp);
+        for (uint32_t ct0 = 0; ct0 < col_tiles; ct0 += D.slab_tiles) {
+            const uint32_t n_ct = col_tiles - ct0 < D.slab_tiles ? col_tiles - ct0 : D.slab_tiles;
+            const uint64_t jobs = (uint64_t)((n_ct + 1) / 2) * row_chunks;
+            const LinearDzCall dz = {a, ct0 == 0 && !dz_apart ? row_chunks * ranges : 0, n, (uint32_t)rows, tok_tiles, P.tiles_per_range, xp};
 #define BOF4_LAUNCH_TURN(OUT_)                                                                                          \
     hipLaunchKernelGGL((linear_turn_kernel<OUT_>),                                                                      \
                        dim3(dz.dz_groups + (uint32_t)((jobs + LINEAR_TURN_WAVES - 1) / LINEAR_TURN_WAVES)),             \
                        dim3(64 * LINEAR_TURN_WAVES), 0, s, (const char*)packed_dev, ct0, n_ct, chunks, row_chunks, cb,  \
                        offsets_dev, entries_dev, (uint32_t)n_outliers, T.lg, T.row_tiles, decoded, dz);
-        if (n_outliers > 0) { BOF4_LAUNCH_TURN(true) } else { BOF4_LAUNCH_TURN(false) }
+            if (n_outliers > 0) { BOF4_LAUNCH_TURN(true) } else { BOF4_LAUNCH_TURN(false) }
 #undef BOF4_LAUNCH_TURN
 #define BOF4_MULTIPLY(TERMS_) \
-    gemm_multiply_decoded<TERMS_>(D, FLUSH, false, decoded, ct0 * GEMM_ROWS, n_ct, cols, TERMS_ * row_chunks, xp, n_tokens, out, s);
-        if (terms == 1) { BOF4_MULTIPLY(1) } else if (terms == 2) { BOF4_MULTIPLY(2) } else { BOF4_MULTIPLY(3) }
+    gemm_multiply_decoded<TERMS_>(D, FLUSH, false, decoded, ct0 * GEMM_ROWS, n_ct, cols, TERMS_ * row_chunks, xp, n, out, s);
+            if (terms == 1) { BOF4_MULTIPLY(1) } else if (terms == 2) { BOF4_MULTIPLY(2) } else { BOF4_MULTIPLY(3) }
 #undef BOF4_MULTIPLY
-    }
-    const uint32_t dbias_groups = l.dbias_dev ? (uint32_t)((rows + 255) / 256) : 0;
-    if (D.split > 1) {
-        const uint32_t dx_groups = (uint32_t)((cols + 1023) / 1024), most = n_tokens < 65535 ? n_tokens : 65535;
-        hipLaunchKernelGGL(linear_sum_kernel, dim3(dx_groups * most + dbias_groups), dim3(256), 0, s, D.split, n_tokens, (uint32_t)cols,
-                           out, dx_groups, most, dbias_parts, P.ranges, (uint32_t)rows, l.dbias_dev);
-    } else if (l.dbias_dev) {
-        hipLaunchKernelGGL(linear_dbias_kernel, dim3(dbias_groups), dim3(256), 0, s, dbias_parts, P.ranges, (uint32_t)rows, l.dbias_dev);
+        }
+        if (D.split > 1) {
+            const uint32_t dx_groups = (uint32_t)((cols + 1023) / 1024), most = n < 65535 ? n : 65535;
+            hipLaunchKernelGGL(linear_sum_kernel, dim3(dx_groups * most + (last ? dbias_groups : 0)), dim3(256), 0, s, D.split, n,
+                               (uint32_t)cols, out, dx_groups, most, dbias_parts, n_parts, (uint32_t)rows, l.dbias_dev);
+        } else if (last && l.dbias_dev) {
+            hipLaunchKernelGGL(linear_dbias_kernel, dim3(dbias_groups), dim3(256), 0, s, dbias_parts, n_parts, (uint32_t)rows, l.dbias_dev);
+        }
+        // the next pass's tokens
+        a.dy = (const char*)a.dy + (uint64_t)n * a.ld_dy * type_bytes(l.dy_type);
+        if (a.pre) a.pre = (const char*)a.pre + (uint64_t)n * a.ld_pre * type_bytes(l.pre_type);
+        if (a.mul) a.mul = (const char*)a.mul + (uint64_t)n * a.ld_mul * type_bytes(l.mul_type);
+        if (a.dmul) a.dmul = (char*)a.dmul + (uint64_t)n * a.ld_dmul * type_bytes(l.dmul_type);
+        if (a.dbias_parts) a.dbias_parts += (uint64_t)ranges * rows;
+        out.token0 += n;
     }
     timing_end(s);
     HIP_TRY(hipGetLastError());

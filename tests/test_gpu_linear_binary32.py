@@ -105,3 +105,34 @@ def test_equal_bits_captured_and_in_a_workspace_of_the_stated_size():
             torch.cuda.synchronize()
             assert torch.equal(dx, m.backward(torch.roll(dy, k, 0), act="silu", pre=pre, out_dtype=out))
         assert torch.equal(m.backward(dy, act="silu", pre=pre, out_dtype=out), want) and bool((whole[size:] == 0xff).all())
+
+
+def test_tokens_in_several_passes():
+    """More tokens than dz's three terms have room for at once (4 GiB): tokens of every pass and around their borders, and dbias of
+    all of them, against binary64; what is written over dy on the way is dmul."""
+    rows, cols, n_tokens = 1 << 18, 96, 5500  # passes of 2688, 2688 and 124 tokens
+    m = Matrix(rows, cols, 0.0005)
+    shape = (n_tokens, rows)
+    dy = torch.empty(shape, dtype=F32, device=DEV)
+    pre, mul = torch.empty(shape, dtype=BF16, device=DEV), torch.empty(shape, dtype=BF16, device=DEV)
+    for t in range(0, n_tokens, 500):
+        dy[t:t + 500], pre[t:t + 500], mul[t:t + 500] = (randn((500, rows), 10 * t + k, F32) for k in range(3))
+    picked = torch.tensor([0, 1, 2687, 2688, 2689, 5375, 5376, 5499], device=DEV)
+    z, f, g = pre[picked].double(), mul[picked].double(), dy[picked].double()
+    a, slope = act64("silu", z)
+    dz, err = g * f * slope, 32 * U * (1 + z.abs()) * (g * f).abs()
+    total, total_abs = torch.zeros(rows, dtype=torch.float64, device=DEV), torch.zeros(rows, dtype=torch.float64, device=DEV)
+    for t in range(0, n_tokens, 500):
+        part = dy[t:t + 500].double() * mul[t:t + 500].double()
+        total_abs += part.abs().mul_(1 + pre[t:t + 500].double().abs()).sum(0)
+        total += part.mul_(act64("silu", pre[t:t + 500].double())[1]).sum(0)
+    dbias = torch.full((rows,), math.nan, device=DEV)
+    dx = m.backward(dy, act="silu", pre=pre, mul=mul, dmul=dy, dbias=dbias, out_dtype=F32)
+    w = m.gemm_w.abs()
+    want, size = dz @ m.gemm_w, dz.abs() @ w
+    assert bool(((dx[picked].double() - want).abs() <= 1.01 * ((3 * rows + 65) * U * size + err @ w + half_step(want, F32))).all())
+    # (and as a whole well below the bound of such long sums: a term of one token lost or taken twice shows)
+    assert float((dx[picked].double() - want).square().mean().sqrt()) <= 512 * U * float(size.square().mean().sqrt())
+    assert bool(((dy[picked].double() - g * a).abs() <= (32 * U * (1 + z.abs()) + 2 * U * a.abs()) * g.abs() + 1.01 * half_step(g * a, F32)).all())
+    # slopes are below 1.2 and off by 32 U (1 + |z|); 5500 binary32 additions in chains of 1 + 32 (and binary64)
+    assert bool(((dbias.double() - total).abs() <= (32 + 1.2 * 64 + 2) * U * total_abs).all())
