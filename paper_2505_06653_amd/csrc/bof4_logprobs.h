@@ -14,6 +14,7 @@
 #include <cstdint>
 
 #include "bof4_device.h"
+#include "bof4_logprobs_plan.h"
 
 namespace bof4 {
 
@@ -166,11 +167,6 @@ __device__ __forceinline__ uint64_t readlane64(uint64_t v, uint32_t lane) {
 // highest 16 bits, by bisection), so that the first tile does not bring a thousand candidates.  Every element that is
 // left out is smaller than `top` others, so the result does not depend on how the row was cut.
 //   With few rows a row is cut into n_splits parts, one per workgroup, whose records logprobs_join_kernel joins.
-constexpr uint32_t LOGPROBS_WORDS = 4, LOGPROBS_JOIN_WAVES = 16; // 16-byte words per lane and tile; waves per row that joins
-constexpr uint32_t LOGPROBS_TILE = 64 * LOGPROBS_WORDS;                // words
-constexpr uint32_t LOGPROBS_MAX_SPLITS = 64;
-constexpr uint32_t logprobs_word_elements(bool bf16) { return bf16 ? 8 : 4; }
-
 struct LogprobsPart {  // what a part of a row leaves: its sums, then `top` keys
     RowSums r;
     uint32_t unused;
@@ -293,7 +289,7 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobsArgs a, ui
         for (uint32_t k = 0; k < LOGPROBS_WORDS; ++k) parked[64 * k + lane] = t.q[k];
         wave_lds_fence();
         for (uint64_t mask = __builtin_amdgcn_ballot_w64(bits != 0u); mask != 0; mask = __builtin_amdgcn_ballot_w64(bits != 0u)) {
-            const uint32_t i = (uint32_t)__builtin_ctz(bits | 0x80000000u), at_word = 64 * (i / PER_WORD) + lane;
+            const uint32_t i = logprobs_lowest(bits, PER_WORD), at_word = logprobs_tile_word(i, lane, PER_WORD);
             const float v = load_logit<BF16>(parked, at_word * PER_WORD + i % PER_WORD);
             const uint32_t place = n_found + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
             if (bits != 0u) found[place] = logit_key(v, (tile * LOGPROBS_TILE + at_word) * PER_WORD + i % PER_WORD - off);

@@ -7,6 +7,7 @@
 #include "bof4_gemm_plan.h"
 #include "bof4_host.h"
 #include "bof4_logprobs.h"
+#include "bof4_logprobs_plan.h"
 
 namespace {
 using namespace bof4;
@@ -14,26 +15,6 @@ using namespace bof4;
 bool valid_type(uint32_t t) { return t == BOF4_F32 || t == BOF4_BF16; }
 size_t type_bytes(uint32_t t) { return t == BOF4_BF16 ? 2 : 4; }
 constexpr uint64_t LOGPROBS_MAX_ROWS = 1ull << 23, LOGPROBS_MAX_VOCAB = 1ull << 30;  // (a launch holds fewer than 2^32 lanes)
-
-// Waves and parts per row.  About 2048 waves keep the chip busy; more of them cost more than they bring, since what a wave does
-// at its row's end is worth a tile or two.  So two waves share a row from 1024 rows on (four where a row of bfloat16 is long: a
-// compute unit holds fewer of those waves, and two leave the last round of workgroups too empty), four from 512 on, and fewer rows
-// are cut into parts of at least a tile per wave for two waves each.  us, one alternative, this / four waves and twice the workgroups:
-// bfloat16 256 x 32000 11.6 / 12.9, 600 x 32000 15.6 / 19.6, 256 x 128000 20.5 / 23.1, binary32 600 x 32000 17.7 / 21.3; 2000 x 128000
-// with two / four waves bfloat16 123 / 103, binary32 187 / 193.
-struct LogprobsCut {
-    uint32_t waves, splits, tiles_per_split;
-};
-LogprobsCut logprobs_cut(uint64_t n_rows, uint64_t vocab, bool bf16) {
-    const uint64_t per_word = logprobs_word_elements(bf16), words = (vocab + 2 * per_word - 2) / per_word;  // wherever it begins
-    const uint64_t tiles = (words + LOGPROBS_TILE - 1) / LOGPROBS_TILE;
-    if (n_rows >= 512) return {n_rows >= 1024 && !(bf16 && tiles >= 48) ? 2u : 4u, 1u, (uint32_t)tiles};
-    uint64_t splits = (1024 + n_rows - 1) / n_rows;
-    if (splits > LOGPROBS_MAX_SPLITS) splits = LOGPROBS_MAX_SPLITS;
-    uint64_t per = (tiles + splits - 1) / splits;
-    if (per < 2) per = 2;
-    return {2, (uint32_t)((tiles + per - 1) / per), (uint32_t)per};
-}
 }  // namespace
 
 extern "C" {
