@@ -218,6 +218,15 @@ def _stream(stream):
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _empty(shape, dtype, device, stream):
+    """A tensor for a call on `stream` (None: the current one), out of that stream's memory: it is not what another stream still
+    works on, and once it is dropped it goes to nobody who does not wait for the call."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def bof4_workspace_bytes(n, block, out_capacity=0):
     return int(lib().bof4_workspace_bytes(n, block, out_capacity))
 
@@ -661,14 +670,19 @@ _F32, _I64, _U8 = (torch.float32,), (torch.int64,), (torch.uint8,)
 
 
 def _scratch(ws, nbytes, device, stream, gpu):
-    """The caller's workspace, or one of `nbytes` that the allocator keeps until `stream` is done with it."""
+    """The caller's workspace, or one of `nbytes`."""
     if ws is not None:
         _flat(ws, "ws", _U8, None, gpu)
         return ws
-    ws = torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
-    if stream is not None:
-        ws.record_stream(stream)
-    return ws
+    return _empty(max(int(nbytes), 1), torch.uint8, device, stream)
+
+
+def _gpu(stream):
+    """The current device, on which the tensors of a call and its stream have to be."""
+    gpu = torch.cuda.current_device()
+    if stream is not None and stream.device_index != gpu:
+        raise ValueError(f"stream must be one of the current GPU: got one of device {stream.device_index}")
+    return gpu
 
 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}  # BOF4_ACT_*
@@ -729,7 +743,7 @@ def bof4_gemv_linear(codes, scales, rows, cols, block, cb, x, table=None, n_outl
     residual, pre, out [n_tokens, rows] (rows of any stride): bfloat16 or float32 each.  act: a key of ACTIVATIONS.  `pre`: a
     tensor that receives x W~^T + bias; `out`: the result's, may be mul or the residual (else of `out_dtype`)."""
     cb, cbp = _cb(cb)
-    gpu = torch.cuda.current_device()
+    gpu = _gpu(stream)
     x2 = _layer_input(x, cols, gpu)
     n_tokens = x2.shape[0]
     table_at, k = _table(table, rows, cols, n_outliers, gpu)
@@ -737,7 +751,7 @@ def bof4_gemv_linear(codes, scales, rows, cols, block, cb, x, table=None, n_outl
             or not codes.is_contiguous() or not scales.is_contiguous() or scales.element_size() != 2:
         raise ValueError("codes and scales (2 bytes each) must be on the current GPU, contiguous, and those of rows x cols weights")
     if out is None:
-        out = torch.empty((n_tokens, rows), dtype=out_dtype, device=x.device)
+        out = _empty((n_tokens, rows), out_dtype, x.device, stream)
     layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out, gpu)
     _check(lib().bof4_gemv_linear(codes.data_ptr(), scales.data_ptr(), rows, cols, block, cbp, table_at, k, x2.data_ptr(),
                                   n_tokens, layer, _stream(stream)))
@@ -753,13 +767,13 @@ def bof4_gemm_linear(packed, rows, cols, cb, x, table=None, n_outliers=0, bias=N
     """y = act(x W^^T + bias) * mul + residual for many tokens; matrix, x, table as for bof4_gemm, the rest as for
     bof4_gemv_linear; `ws`: optional uint8 device tensor of bof4_gemm_linear_workspace_bytes(...) bytes."""
     cb, cbp = _cb(cb)
-    gpu = torch.cuda.current_device()
+    gpu = _gpu(stream)
     x2 = _layer_input(x, cols, gpu)
     packed_at = _packed(packed, rows, cols, gpu)
     n_tokens = x2.shape[0]
     table_at, k = _table(table, rows, cols, n_outliers, gpu)
     if out is None:
-        out = torch.empty((n_tokens, rows), dtype=out_dtype, device=x.device)
+        out = _empty((n_tokens, rows), out_dtype, x.device, stream)
     layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out, gpu)
     ws = _scratch(ws, 0 if ws is not None else bof4_gemm_linear_workspace_bytes(rows, cols, n_tokens), x.device, stream, gpu)
     _check(lib().bof4_gemm_linear(packed_at, rows, cols, cbp, table_at, k, x2.data_ptr(), n_tokens, layer, ws.data_ptr(),
@@ -780,11 +794,11 @@ def bof4_gemm_linear_backward(packed, rows, cols, cb, dy, table=None, n_outliers
     cb, cbp = _cb(cb)
     if dy.dim() != 2 or dy.shape[1] != rows:
         raise ValueError("dy must be [n_tokens, rows]")
-    gpu, n_tokens = torch.cuda.current_device(), dy.shape[0]
+    gpu, n_tokens = _gpu(stream), dy.shape[0]
     packed_at = _packed(packed, rows, cols, gpu)
     table_at, k = _table(table, rows, cols, n_outliers, gpu)
     if out is None:
-        out = torch.empty((n_tokens, cols), dtype=out_dtype, device=dy.device)
+        out = _empty((n_tokens, cols), out_dtype, dy.device, stream)
     shape = (n_tokens, rows)
     pre_at = mul_at = dmul_at = dbias_at = pre_type = mul_type = dmul_type = ld_pre = ld_mul = ld_dmul = 0
     dy_at, dx_at = _tensor(dy, "dy", _TYPES, shape, gpu), _tensor(out, "out", _TYPES, (n_tokens, cols), gpu)
@@ -812,18 +826,19 @@ def bof4_token_logprobs(logits, targets=None, top=0, ws=None, stream=None):
     """logits: float32 or bfloat16 [n_rows, vocab] on the device, rows of any stride; targets: int64 [n_rows] (below 0: no
     token asked for).  Returns (logprob float32 [n_rows] or None without targets, entropy float32 [n_rows], top_idx int64
     [n_rows, top] and top_logprob float32 [n_rows, top] or None with top = 0, stats float32 [n_rows, 2])."""
-    gpu = torch.cuda.current_device()
+    gpu = _gpu(stream)
     logits_at = _tensor(logits, "logits", _TYPES, None, gpu)
     if logits.dim() != 2:
         raise ValueError("logits must be [n_rows, vocab]")
     n, vocab = logits.shape
-    f32, top, new = torch.float32, int(top), logits.new_empty
+    f32, top = torch.float32, int(top)
+    new = logits.new_empty if stream is None else lambda shape, dtype: _empty(shape, dtype, logits.device, stream)
     if top < 0:
         raise ValueError("top must not be negative")
     logprob = top_idx = top_logprob = targets_at = logprob_at = idx_at = top_at = None
     stats, entropy = new((n, 2), dtype=f32), new(n, dtype=f32)
     if targets is not None:
-        targets_at, logprob = _flat(targets, "targets", _I64, (n,), gpu), torch.empty_like(entropy)
+        targets_at, logprob = _flat(targets, "targets", _I64, (n,), gpu), new(n, dtype=f32)
         logprob_at = logprob.data_ptr()
     if top > 0:
         top_idx, top_logprob = new((n, top), dtype=torch.int64), new((n, top), dtype=f32)
@@ -839,7 +854,7 @@ def bof4_token_logprobs_backward(logits, stats, targets=None, d_logprob=None, en
                                  out_dtype=None, stream=None):
     """The gradient by the logits, [n_rows, vocab], from bof4_token_logprobs' stats (and entropy) and the gradients of its
     logprob and entropy (float32 [n_rows]; None: that output is not used).  `out`: a tensor to fill, may be the logits."""
-    gpu = torch.cuda.current_device()
+    gpu = _gpu(stream)
     logits_at = _tensor(logits, "logits", _TYPES, None, gpu)
     if logits.dim() != 2:
         raise ValueError("logits must be [n_rows, vocab]")
@@ -852,7 +867,7 @@ def bof4_token_logprobs_backward(logits, stats, targets=None, d_logprob=None, en
     if entropy is not None:
         entropy_at, d_entropy_at = _flat(entropy, "entropy", _F32, (n,), gpu), _flat(d_entropy, "d_entropy", _F32, (n,), gpu)
     if out is None:
-        out = torch.empty((n, vocab), dtype=out_dtype or logits.dtype, device=logits.device)
+        out = _empty((n, vocab), out_dtype or logits.dtype, logits.device, stream)
     out_at = _tensor(out, "out", _TYPES, (n, vocab), gpu)
     _check(lib().bof4_token_logprobs_backward(logits_at, _TYPES[logits.dtype], n, vocab, _row_stride(logits),
                                               _flat(stats, "stats", _F32, (n, 2), gpu), targets_at, d_logprob_at, entropy_at,
