@@ -227,6 +227,15 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _result(shape, dtype, device, stream):
+    """The same for a result: the caller works with it on the current stream as well, which has to be done with it, too, before
+    the memory of a dropped one is used again."""
+    t = _empty(shape, dtype, device, stream)
+    if stream is not None:
+        t.record_stream(torch.cuda.current_stream())
+    return t
+
+
 def bof4_workspace_bytes(n, block, out_capacity=0):
     return int(lib().bof4_workspace_bytes(n, block, out_capacity))
 
@@ -751,7 +760,7 @@ def bof4_gemv_linear(codes, scales, rows, cols, block, cb, x, table=None, n_outl
             or not codes.is_contiguous() or not scales.is_contiguous() or scales.element_size() != 2:
         raise ValueError("codes and scales (2 bytes each) must be on the current GPU, contiguous, and those of rows x cols weights")
     if out is None:
-        out = _empty((n_tokens, rows), out_dtype, x.device, stream)
+        out = _result((n_tokens, rows), out_dtype, x.device, stream)
     layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out, gpu)
     _check(lib().bof4_gemv_linear(codes.data_ptr(), scales.data_ptr(), rows, cols, block, cbp, table_at, k, x2.data_ptr(),
                                   n_tokens, layer, _stream(stream)))
@@ -773,7 +782,7 @@ def bof4_gemm_linear(packed, rows, cols, cb, x, table=None, n_outliers=0, bias=N
     n_tokens = x2.shape[0]
     table_at, k = _table(table, rows, cols, n_outliers, gpu)
     if out is None:
-        out = _empty((n_tokens, rows), out_dtype, x.device, stream)
+        out = _result((n_tokens, rows), out_dtype, x.device, stream)
     layer = _layer(n_tokens, rows, bias, act, mul, residual, pre, out, gpu)
     ws = _scratch(ws, 0 if ws is not None else bof4_gemm_linear_workspace_bytes(rows, cols, n_tokens), x.device, stream, gpu)
     _check(lib().bof4_gemm_linear(packed_at, rows, cols, cbp, table_at, k, x2.data_ptr(), n_tokens, layer, ws.data_ptr(),
@@ -798,7 +807,7 @@ def bof4_gemm_linear_backward(packed, rows, cols, cb, dy, table=None, n_outliers
     packed_at = _packed(packed, rows, cols, gpu)
     table_at, k = _table(table, rows, cols, n_outliers, gpu)
     if out is None:
-        out = _empty((n_tokens, cols), out_dtype, dy.device, stream)
+        out = _result((n_tokens, cols), out_dtype, dy.device, stream)
     shape = (n_tokens, rows)
     pre_at = mul_at = dmul_at = dbias_at = pre_type = mul_type = dmul_type = ld_pre = ld_mul = ld_dmul = 0
     dy_at, dx_at = _tensor(dy, "dy", _TYPES, shape, gpu), _tensor(out, "out", _TYPES, (n_tokens, cols), gpu)
@@ -832,7 +841,7 @@ def bof4_token_logprobs(logits, targets=None, top=0, ws=None, stream=None):
         raise ValueError("logits must be [n_rows, vocab]")
     n, vocab = logits.shape
     f32, top = torch.float32, int(top)
-    new = logits.new_empty if stream is None else lambda shape, dtype: _empty(shape, dtype, logits.device, stream)
+    new = logits.new_empty if stream is None else lambda shape, dtype: _result(shape, dtype, logits.device, stream)
     if top < 0:
         raise ValueError("top must not be negative")
     logprob = top_idx = top_logprob = targets_at = logprob_at = idx_at = top_at = None
@@ -867,7 +876,7 @@ def bof4_token_logprobs_backward(logits, stats, targets=None, d_logprob=None, en
     if entropy is not None:
         entropy_at, d_entropy_at = _flat(entropy, "entropy", _F32, (n,), gpu), _flat(d_entropy, "d_entropy", _F32, (n,), gpu)
     if out is None:
-        out = _empty((n, vocab), out_dtype or logits.dtype, logits.device, stream)
+        out = _result((n, vocab), out_dtype or logits.dtype, logits.device, stream)
     out_at = _tensor(out, "out", _TYPES, (n, vocab), gpu)
     _check(lib().bof4_token_logprobs_backward(logits_at, _TYPES[logits.dtype], n, vocab, _row_stride(logits),
                                               _flat(stats, "stats", _F32, (n, 2), gpu), targets_at, d_logprob_at, entropy_at,

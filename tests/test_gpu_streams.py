@@ -117,3 +117,28 @@ def test_a_side_stream_inside_a_capture():
         torch.cuda.synchronize()
         for a, b in zip(got, binding.bof4_token_logprobs(torch.roll(logits, k, 1), t, top=9)):
             assert torch.equal(a, b)
+
+
+def check_dropped(call):
+    """Results that the current stream still reads when they are dropped: the call's stream does not write there again before that
+    is done."""
+    work, main, side = randn((4096, 4096), 1), torch.cuda.current_stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    results = call(side)
+    main.wait_stream(side)
+    for _ in range(300):
+        work @ work
+    for r in results:
+        r.clone()
+    places, reading = spans(results), torch.cuda.Event()
+    reading.record()
+    del results
+    again = call(side)
+    if not reading.query():  # (the current stream was still at work when memory was found for the second call)
+        assert not meet(spans(again), places)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("which", range(5), ids=NAMES)
+def test_dropped_results_are_left_alone_until_the_current_stream_has_read_them(which):
+    check_dropped(calls()[which][1])
