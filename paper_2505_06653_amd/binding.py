@@ -287,7 +287,7 @@ def bof4_theory_centroids(pdf, cdf, u_max, block, cb, pinned_mask, signed, ws=No
     cb, cbp = _cb(cb)
     n = int(pdf.size)
     if ws is None:
-        ws = torch.empty(int(lib().bof4_theory_workspace_bytes(n)), dtype=torch.uint8, device=device)
+        ws = _empty(int(lib().bof4_theory_workspace_bytes(n)), torch.uint8, device, stream)
     out = np.zeros(16, dtype=np.float64)
     _check(lib().bof4_theory_centroids(pdf.ctypes.data_as(_F64P), cdf.ctypes.data_as(_F64P), n, float(u_max), block,
                                        cbp, int(pinned_mask), int(signed), out.ctypes.data_as(_F64P), _ptr(ws),
@@ -301,9 +301,10 @@ def bof4_time_next_call(start_event, stop_event):
     _check(lib().bof4_time_next_call(ctypes.c_void_p(start_event.cuda_event), ctypes.c_void_p(stop_event.cuda_event)))
 
 
-def alloc_workspace(n, block, out_capacity=0, device="cuda"):
+def alloc_workspace(n, block, out_capacity=0, device="cuda", stream=None):
+    """A workspace for calls on `stream` (default: the current one)."""
     nbytes = max(bof4_workspace_bytes(n, block, out_capacity), 256)
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _empty(nbytes, torch.uint8, device, stream)
 
 
 def pinned_lloyd_stats():
@@ -335,7 +336,7 @@ def bof4_quant_error(w, block, cb, signed, opq_T=0.0, ws=None, stream=None, out=
     cb, cbp = _cb(cb)
     n = w.numel()
     if ws is None:
-        ws = alloc_workspace(n, block, 0, w.device)
+        ws = alloc_workspace(n, block, 0, w.device, stream)
     rec = out if out is not None else ErrorStats()
     _check(lib().bof4_quant_error(_ptr(w), n, block, cbp, int(signed), float(opq_T), ctypes.byref(rec), _ptr(ws),
                                   ws.numel(), _stream(stream)))
@@ -356,7 +357,7 @@ def bof4_gemv_outlier_table(codes, scales, rows, cols, block, cb, out_idx, out_v
             raise ValueError("n_outliers exceeds the list")
         k = int(n_outliers)
     if out is None:
-        out = torch.empty(bof4_gemv_outlier_table_bytes(rows, cols, k), dtype=torch.uint8, device=codes.device)
+        out = _result(bof4_gemv_outlier_table_bytes(rows, cols, k), torch.uint8, codes.device, stream)
     _check(lib().bof4_gemv_outlier_table(_ptr(codes), _ptr(scales), rows, cols, block, cbp,
                                          _ptr(out_idx) if k else None, _ptr(out_val) if k else None, k, _ptr(out),
                                          out.numel(), _stream(stream)))
@@ -372,7 +373,7 @@ def bof4_gemv(codes, scales, rows, cols, block, cb, x, table=None, n_outliers=0,
         raise ValueError("x must be a contiguous bfloat16 tensor of [n_tokens, cols]")
     n_tokens = int(x2.shape[0])
     if out is None:
-        out = torch.empty((n_tokens, rows), dtype=torch.float32, device=x.device)
+        out = _result((n_tokens, rows), torch.float32, x.device, stream)
     k = int(n_outliers)
     if k and table is None:
         raise ValueError("outliers need their table (bof4_gemv_outlier_table)")
@@ -395,7 +396,7 @@ def bof4_gemm_outlier_table(codes, scales, rows, cols, block, cb, out_idx, out_v
             raise ValueError("n_outliers exceeds the list")
         k = int(n_outliers)
     if out is None:
-        out = torch.empty(bof4_gemv_outlier_table_bytes(rows, cols, k), dtype=torch.uint8, device=codes.device)
+        out = _result(bof4_gemv_outlier_table_bytes(rows, cols, k), torch.uint8, codes.device, stream)
     _check(lib().bof4_gemm_outlier_table(_ptr(codes), _ptr(scales), rows, cols, block, cbp,
                                          _ptr(out_idx) if k else None, _ptr(out_val) if k else None, k, _ptr(out),
                                          out.numel(), _stream(stream)))
@@ -410,7 +411,7 @@ def bof4_gemm_pack(codes, scales, rows, cols, block, out=None, stream=None):
     """Codes and block constants of one quantised matrix in the order bof4_gemm reads them (uint8 device tensor;
     made once)."""
     if out is None:
-        out = torch.empty(bof4_gemm_packed_bytes(rows, cols), dtype=torch.uint8, device=codes.device)
+        out = _result(bof4_gemm_packed_bytes(rows, cols), torch.uint8, codes.device, stream)
     _check(lib().bof4_gemm_pack(_ptr(codes), _ptr(scales), rows, cols, block, _ptr(out), out.numel(), _stream(stream)))
     return out
 
@@ -428,12 +429,12 @@ def bof4_gemm(packed, rows, cols, cb, x, table=None, n_outliers=0, out=None, ws=
         raise ValueError("packed matrix too small for rows x cols (bof4_gemm_pack)")
     n_tokens = int(x2.shape[0])
     if out is None:
-        out = torch.empty((n_tokens, rows), dtype=torch.float32, device=x.device)
+        out = _result((n_tokens, rows), torch.float32, x.device, stream)
     k = int(n_outliers)
     if k and table is None:
         raise ValueError("outliers need their table (bof4_gemm_outlier_table)")
     if ws is None:
-        ws = torch.empty(bof4_gemm_workspace_bytes(rows, cols, n_tokens), dtype=torch.uint8, device=x.device)
+        ws = _empty(bof4_gemm_workspace_bytes(rows, cols, n_tokens), torch.uint8, x.device, stream)
     _check(lib().bof4_gemm(_ptr(packed), rows, cols, cbp, _ptr(table) if k else None, k, _ptr(x2), n_tokens,
                            _ptr(out), _ptr(ws), ws.numel(), _stream(stream)))
     return out
@@ -446,7 +447,7 @@ def bof4_lloyd_step(w, block, cb, signed, opq_T=0.0, weight_by_max2=True, ws=Non
     n = w.numel()
     cb, cbp = _cb(cb)
     if ws is None:
-        ws = alloc_workspace(n, block, 0, w.device)
+        ws = alloc_workspace(n, block, 0, w.device, stream)
     if out is None:
         out = LloydStats()
     _check(lib().bof4_lloyd_step(_ptr(w), n, block, cbp, int(signed), float(opq_T), int(bool(weight_by_max2)),
@@ -462,7 +463,7 @@ def bof4_lloyd_step_mae(w, block, cb, signed, opq_T=0.0, skip_mask=0, ws=None, s
     n = w.numel()
     cb, cbp = _cb(cb)
     if ws is None:
-        ws = alloc_workspace(n, block, 0, w.device)
+        ws = alloc_workspace(n, block, 0, w.device, stream)
     if out is None:
         out = MaeStats()
     _check(lib().bof4_lloyd_step_mae(_ptr(w), n, block, cbp, int(signed), float(opq_T), int(bool(weight_by_max)),
@@ -496,16 +497,16 @@ def bof4_quantize(w, block, cb, signed, opq_T=0.0, out_capacity=0, codes=None, s
     dev = w.device
     cb, cbp = _cb(cb)
     if codes is None:
-        codes = torch.empty(max(n // 2, 1), dtype=torch.uint8, device=dev)
+        codes = _result(max(n // 2, 1), torch.uint8, dev, stream)
     if scales is None:
-        scales = torch.empty(max(n // max(block, 1), 1), dtype=torch.float16, device=dev)
+        scales = _result(max(n // max(block, 1), 1), torch.float16, dev, stream)
     if opq_T > 0:
         if out_idx is None:
-            out_idx = torch.empty(max(out_capacity, 1), dtype=torch.int64, device=dev)
+            out_idx = _result(max(out_capacity, 1), torch.int64, dev, stream)
         if out_val is None:
-            out_val = torch.empty(max(out_capacity, 1), dtype=torch.float16, device=dev)
+            out_val = _result(max(out_capacity, 1), torch.float16, dev, stream)
         if ws is None:
-            ws = alloc_workspace(n, block, out_capacity, dev)
+            ws = alloc_workspace(n, block, out_capacity, dev, stream)
     nout = counter if counter is not None else ctypes.c_uint64(0)
     code = lib().bof4_quantize(_ptr(w), n, block, cbp, int(signed), float(opq_T), _ptr(codes), _ptr(scales),
                                _ptr(out_idx), _ptr(out_val), out_capacity, ctypes.byref(nout), _ptr(ws),
@@ -528,16 +529,16 @@ def bof4_quantize_lloyd(w, block, cb, signed, opq_T=0.0, out_capacity=0, weight_
     dev = w.device
     cb, cbp = _cb(cb)
     if codes is None:
-        codes = torch.empty(max(n // 2, 1), dtype=torch.uint8, device=dev)
+        codes = _result(max(n // 2, 1), torch.uint8, dev, stream)
     if scales is None:
-        scales = torch.empty(max(n // max(block, 1), 1), dtype=torch.float16, device=dev)
+        scales = _result(max(n // max(block, 1), 1), torch.float16, dev, stream)
     if opq_T > 0:
         if out_idx is None:
-            out_idx = torch.empty(max(out_capacity, 1), dtype=torch.int64, device=dev)
+            out_idx = _result(max(out_capacity, 1), torch.int64, dev, stream)
         if out_val is None:
-            out_val = torch.empty(max(out_capacity, 1), dtype=torch.float16, device=dev)
+            out_val = _result(max(out_capacity, 1), torch.float16, dev, stream)
     if ws is None:
-        ws = alloc_workspace(n, block, out_capacity, dev)
+        ws = alloc_workspace(n, block, out_capacity, dev, stream)
     nout = counter if counter is not None else ctypes.c_uint64(0)
     st = stats if stats is not None else LloydStats()
     code = lib().bof4_quantize_lloyd(_ptr(w), n, block, cbp, int(signed), float(opq_T), int(bool(weight_by_max2)),
@@ -609,7 +610,7 @@ def bof4_lloyd_step_begin(w, block, cb, signed, out, opq_T=0.0, weight_by_max2=T
     n = w.numel()
     cb, cbp = _cb(cb)
     if ws is None:
-        ws = alloc_workspace(n, block, 0, w.device)
+        ws = alloc_workspace(n, block, 0, w.device, stream)
     _check(lib().bof4_lloyd_step_begin(_ptr(w), n, block, cbp, int(signed), float(opq_T), int(bool(weight_by_max2)),
                                        ctypes.byref(out), _ptr(ws), ws.numel(), _stream(stream)))
     return out
@@ -639,7 +640,7 @@ def bof4_dequantize(codes, scales, n, block, cb, out_idx=None, out_val=None, out
     entries of out_idx / out_val (all of them if n_outliers is None)."""
     cb, cbp = _cb(cb)
     if out is None:
-        out = torch.empty(n, dtype=torch.bfloat16, device=codes.device)
+        out = _result(n, torch.bfloat16, codes.device, stream)
     k = 0 if out_idx is None else int(out_idx.numel())
     if n_outliers is not None:
         if n_outliers > k:

@@ -142,3 +142,39 @@ def check_dropped(call):
 @pytest.mark.parametrize("which", range(5), ids=NAMES)
 def test_dropped_results_are_left_alone_until_the_current_stream_has_read_them(which):
     check_dropped(calls()[which][1])
+
+
+def codec_calls():
+    """The same of the codec's and the products' calls (those that return numbers of the host: no tensors)."""
+    m = Matrix(1001, 2080, 0.01)
+    w = randn(1001 * 2080, 1, scale=0.02)
+    n, block, cb = w.numel(), 32, m.cb
+    T = binding.bof4_opq_threshold(0.95, block)
+    codes, scales, oi, ov, k = binding.bof4_quantize(w, block, cb, 1, opq_T=T, out_capacity=n // 20)
+    x, few = randn((300, 2080), 1), randn((3, 2080), 2)
+    args = (codes, scales, 1001, 2080, block, cb, oi, ov)
+    return {
+        "quantize": lambda s: list(binding.bof4_quantize(w, block, cb, 1, opq_T=T, out_capacity=n // 20, stream=s, trim=False)[:4]),
+        "quantize_lloyd": lambda s: list(binding.bof4_quantize_lloyd(w, block, cb, 1, opq_T=T, out_capacity=n // 20, stream=s, trim=False)[:4]),
+        "dequantize": lambda s: [binding.bof4_dequantize(codes, scales, n, block, cb, oi, ov, stream=s)],
+        "gemv_outlier_table": lambda s: [binding.bof4_gemv_outlier_table(*args, stream=s)],
+        "gemm_outlier_table": lambda s: [binding.bof4_gemm_outlier_table(*args, stream=s)],
+        "gemm_pack": lambda s: [binding.bof4_gemm_pack(codes, scales, 1001, 2080, block, stream=s)],
+        "gemv": lambda s: [binding.bof4_gemv(m.codes, m.scales, 1001, 2080, 32, cb, few, m.gemv_table, m.k, stream=s)],
+        "gemm": lambda s: [binding.bof4_gemm(m.packed, 1001, 2080, cb, x, m.gemm_table, m.k, stream=s)],
+        "lloyd_step": lambda s: [] if binding.bof4_lloyd_step(w, block, cb, 1, opq_T=T, stream=s) else None,
+        "lloyd_step_mae": lambda s: [] if binding.bof4_lloyd_step_mae(w, block, cb, 1, opq_T=T, stream=s) else None,
+        "quant_error": lambda s: [] if binding.bof4_quant_error(w, block, cb, 1, opq_T=T, stream=s) else None,
+    }
+
+
+CODEC = ["quantize", "quantize_lloyd", "dequantize", "gemv_outlier_table", "gemm_outlier_table", "gemm_pack", "gemv", "gemm", "lloyd_step",
+         "lloyd_step_mae", "quant_error"]
+
+
+@pytest.mark.parametrize("name", CODEC)
+def test_memory_of_the_codec_s_and_the_products_calls_is_their_stream_s(monkeypatch, name):
+    call = codec_calls()[name]
+    call(None)
+    check_places(monkeypatch, call)
+    check_dropped(call)
