@@ -82,7 +82,7 @@ __device__ __forceinline__ void finish_row(const LogprobsArgs& a, uint32_t row, 
         }
         if (a.entropy) a.entropy[row] = nothing ? 0.0f : log_s - r.t / r.s;
         if (a.stats) {
-            a.stats[2 * (uint64_t)row] = r.m;
+            a.stats[2 * (uint64_t)row] = r.s != r.s ? r.s : r.m;  // (the maximum passes NaN over)
             a.stats[2 * (uint64_t)row + 1] = log_s;
         }
     }
