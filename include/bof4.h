@@ -477,8 +477,8 @@ size_t bof4_token_logprobs_workspace_bytes(uint64_t n_rows, uint64_t vocab, uint
  *   entropy_dev and d_entropy_dev  both, or neither (then h = 0); entropy as bof4_token_logprobs wrote it
  *   d_logits_dev  n_rows x vocab of d_logits_type, row stride ld_d_logits (>= vocab), all of it written; may be the logits
  *               themselves (one type and one row stride), else apart from them
- * A logit of -inf and a row of nothing else have a gradient of 0 (the target's own part g aside); a row with a NaN or +inf
- * has NaN.  Limits as above, and fewer than 2^24 stretches of 2048 logits.  Only enqueues.
+ * A logit of -inf has a gradient of 0 (the target's own part g aside), a row of nothing else 0 throughout; a row with a NaN or
+ * +inf has NaN.  Limits as above, and fewer than 2^24 stretches of 2048 logits.  Only enqueues.
  */
 int bof4_token_logprobs_backward(const void* logits_dev, uint32_t logits_type, uint64_t n_rows, uint64_t vocab,
                                  uint64_t ld_logits, const float* stats_dev, const int64_t* target_dev,

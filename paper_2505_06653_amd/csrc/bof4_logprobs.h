@@ -476,7 +476,8 @@ __global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobsGradArgs a, 
     const float ms = finite_max(m);
     auto slope = [&](float x) __attribute__((always_inline)) {
         const float lp = (x - ms) - log_s, p = logprobs_exp(lp);
-        return ENTROPY ? -p * fmaf(h, fmaxf(lp, LOGPROBS_FAR) + H, g) : -p * g;
+        // (p times log p first: with a large h their product is what is finite)
+        return ENTROPY ? -fmaf(p * (fmaxf(lp, LOGPROBS_FAR) + H), h, p * g) : -p * g;
     };
     auto one = [&](uint32_t j) {  // j counted from the first word, as `target`
         const float x = load_logit<BF16>(words, j);

@@ -31,3 +31,29 @@ def test_every_value_of_a_row_with_a_nan_or_inf_is_nan(dtype, n, vocab, top):
     g = torch.ones(n, device=DEV)
     d = binding.bof4_token_logprobs_backward(x, stats, t, g, h, g)
     assert bool(d[bad].isnan().all()) and bool(d[good].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("h", [3.4e38, -3.4e38, 1e36, 1e30])
+def test_gradients_of_the_entropy_up_to_the_largest_number(dtype, out, h):
+    """d = -h p (log p + H): p is small where log p is large, so what is finite by the formula has to come out so, and 0 where
+    there is no probability."""
+    x = torch.full((2, 2003), -math.inf, device=DEV)
+    x[:, ::5] = torch.linspace(-80, -20, 401, device=DEV)
+    x[:, 7], x[:, 9], x[0, 11], x[:, 12] = 0.0, -1e30, -1.5, torch.finfo(dtype).min
+    x = x.to(dtype)
+    _, H, _, _, stats = binding.bof4_token_logprobs(x)
+    hs, g, t = torch.full((2,), h, device=DEV), torch.ones(2, device=DEV), torch.full((2,), 7, device=DEV)
+    for args in ((None, None), (t, g)):
+        d = binding.bof4_token_logprobs_backward(x, stats, *args, H, hs, out_dtype=out)
+        lp = torch.log_softmax(x.double(), -1)
+        p = lp.exp()
+        safe = torch.where(p > 0, lp, 0.0)
+        want = -float(hs[0]) * p * (safe + H.double()[:, None])
+        # lp, of up to 80, and H are off by 2^-24 of 80 each, and so is p: 2^-15 of what is summed up, generously (and of 1: S, a
+        # little above 1, is off by 2^-24 at least, and with it log S, however small it is); p below 2^-126 may be 0
+        tol = abs(float(hs[0])) * (p * (safe.abs() + H.double()[:, None] + 1) * 2.0 ** -15 + p.clamp(max=2.0 ** -126) * 200) + 2.0
+        tol = tol + (want.abs() * 2.0 ** -8 if out == torch.bfloat16 else 0.0)
+        assert bool(d.isfinite().all()) and bool(((d.double() - want).abs() <= tol).all())
+        assert bool((d[:, 1] == 0).all()) and bool((d[:, 9] == 0).all()) and bool((d[:, 12] == 0).all())
