@@ -364,13 +364,19 @@ def bof4_gemv_outlier_table(codes, scales, rows, cols, block, cb, out_idx, out_v
     return out
 
 
+def _tokens(x, cols):
+    """x as [n_tokens, cols]; one token may come as [cols]."""
+    x2 = x[None, :] if x.dim() == 1 else x
+    if x2.dim() != 2 or x2.dtype != torch.bfloat16 or x2.shape[1] != cols or not x2.is_contiguous():
+        raise ValueError("x must be a contiguous bfloat16 tensor of [n_tokens, cols]")
+    return x2
+
+
 def bof4_gemv(codes, scales, rows, cols, block, cb, x, table=None, n_outliers=0, out=None, stream=None):
     """y = x W~^T for the quantised row-major [rows, cols] matrix; x is bf16 [n_tokens, cols] (or [cols]) on the
     device, the result float32 [n_tokens, rows].  `table` (bof4_gemv_outlier_table) brings n_outliers outliers in."""
     cb, cbp = _cb(cb)
-    x2 = x if x.dim() == 2 else x[None, :]
-    if x2.dtype != torch.bfloat16 or x2.shape[1] != cols or not x2.is_contiguous():
-        raise ValueError("x must be a contiguous bfloat16 tensor of [n_tokens, cols]")
+    x2 = _tokens(x, cols)
     n_tokens = int(x2.shape[0])
     if out is None:
         out = _result((n_tokens, rows), torch.float32, x.device, stream)
@@ -422,9 +428,7 @@ def bof4_gemm(packed, rows, cols, cb, x, table=None, n_outliers=0, out=None, ws=
     (bof4_gemm_outlier_table) brings n_outliers outliers in; `ws`: optional uint8 device tensor of
     bof4_gemm_workspace_bytes(...) bytes."""
     cb, cbp = _cb(cb)
-    x2 = x if x.dim() == 2 else x[None, :]
-    if x2.dtype != torch.bfloat16 or x2.shape[1] != cols or not x2.is_contiguous():
-        raise ValueError("x must be a contiguous bfloat16 tensor of [n_tokens, cols]")
+    x2 = _tokens(x, cols)
     if packed.numel() < bof4_gemm_packed_bytes(rows, cols):
         raise ValueError("packed matrix too small for rows x cols (bof4_gemm_pack)")
     n_tokens = int(x2.shape[0])
@@ -705,9 +709,9 @@ def _activation(act):
 
 
 def _layer_input(x, cols, gpu):
-    x2 = x if x.dim() == 2 else x[None, :]
-    if x2.dtype != torch.bfloat16 or x2.shape[1] != cols or not x2.is_contiguous() or x2.get_device() != gpu:
-        raise ValueError("x must be a contiguous bfloat16 tensor of [n_tokens, cols] on the current GPU")
+    x2 = _tokens(x, cols)
+    if x2.get_device() != gpu:
+        raise ValueError("x must be on the current GPU")
     return x2
 
 
