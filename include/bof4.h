@@ -32,11 +32,11 @@ extern "C" {
 #define BOF4_ERR_WORKSPACE (-3) /* ws_bytes below bof4_workspace_bytes(...)                                    */
 #define BOF4_ERR_HIP (-4)       /* a HIP runtime call failed                                                   */
 
-/* Per-region sums of one Lloyd / EM expectation pass (section 3.2 eq. 6; appendix B.3). */
 /* Element types of tensors that may come in more than one. */
 #define BOF4_F32 0u
 #define BOF4_BF16 1u
 
+/* Per-region sums of one Lloyd / EM expectation pass (section 3.2 eq. 6; appendix B.3). */
 typedef struct {
     double num[16];      /* sum over region l of g * x      (numerator of eq. 6)                               */
     double den[16];      /* sum over region l of g          (denominator of eq. 6)                             */
