@@ -53,8 +53,6 @@ __device__ __forceinline__ float key_logit(uint64_t key) {
     return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
 }
 __device__ __forceinline__ uint32_t key_id(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
-// an alternative: neither NaN nor without probability
-__device__ __forceinline__ bool is_alternative(float x) { return x > -INFINITY; }
 
 struct LogprobsArgs {
     const void* logits;
@@ -249,7 +247,8 @@ __global__ __launch_bounds__(64 * WAVES) void logprobs_kernel(LogprobsArgs a, ui
 
     float m = -INFINITY, s0 = 0.0f, s1 = 0.0f, t0 = 0.0f, t1 = 0.0f;
     uint64_t list = 0;                     // the wave's best, descending over the lanes
-    float bound = -3.4028234663852886e38f;  // what a logit has to reach to matter (the lowest number: any but -inf)
+    // What a logit has to reach to be an alternative: at first the lowest number, which -inf and NaN do not.
+    float bound = -3.4028234663852886e38f;
     float last_of_list = bound;             // the `top`-th best so far
     uint32_t n_found = 0;
     uint64_t* found = sh.found[wave];
