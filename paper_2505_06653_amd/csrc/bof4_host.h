@@ -49,6 +49,8 @@ inline bool valid_codebook(const double* cb) {
         if (!(cb[l] > cb[l - 1])) return false;
     return true;
 }
+inline bool valid_type(uint32_t t) { return t == BOF4_F32 || t == BOF4_BF16; }
+inline size_t type_bytes(uint32_t t) { return t == BOF4_BF16 ? 2 : 4; }
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 inline void make_thresholds(const double* cb, float* thr) {

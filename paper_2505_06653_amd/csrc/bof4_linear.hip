@@ -16,8 +16,6 @@ namespace {
 using namespace bof4;
 
 constexpr uint64_t LINEAR_MAX_ROWS = 1ull << 30, LINEAR_BACKWARD_MAX_ROWS = 1ull << 18;
-bool valid_type(uint32_t t) { return t == BOF4_F32 || t == BOF4_BF16; }
-size_t type_bytes(uint32_t t) { return t == BOF4_BF16 ? 2 : 4; }
 
 // A tensor of tokens x rows as a call names it.
 struct Rows {

@@ -12,8 +12,6 @@
 namespace {
 using namespace bof4;
 
-bool valid_type(uint32_t t) { return t == BOF4_F32 || t == BOF4_BF16; }
-size_t type_bytes(uint32_t t) { return t == BOF4_BF16 ? 2 : 4; }
 constexpr uint64_t LOGPROBS_MAX_ROWS = 1ull << 23, LOGPROBS_MAX_VOCAB = 1ull << 30;  // (a launch holds fewer than 2^32 lanes)
 }  // namespace
 
