@@ -2,6 +2,12 @@
 
 torch supplies device memory (tensors) and the stream; nothing is computed here.  The functions carry the names of
 the C entry points.  A missing library is an error (there is no fallback of any kind).
+
+`stream` of a call is the torch.cuda.Stream that it enqueues on (default: the current one).  What the call allocates belongs to
+that stream; the caller sees to it that its own tensors are ready there and that they live until the call is done with them.
+The calls know nothing of autograd: what they return carries no graph, whatever their inputs require.  A
+torch.autograd.Function joins a call and its gradient (its backward gets the tensors that the forward call wrote: pre, stats,
+entropy).
 """
 import ctypes
 import os
