@@ -417,8 +417,8 @@ size_t bof4_gemm_linear_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t n
  *     dz = dy * mul * act'(pre),   dx = dz W^,   dmul = dy * act(pre),   dbias = sum over the tokens of dz
  * (and the residual's gradient is dy itself), W^ the bfloat16 matrix of bof4_gemm from its packed copy and table.  The types
  * of dy and dx say how much of dz goes into the sums of dx: with both in bfloat16 dz is rounded to bfloat16 (2^-8 of itself at
- * most), with dy in binary32 and dx in bfloat16 it is held in sixteen bits (2^-16), and with dx in binary32 in all its 24 (two
- * and three products take as much longer).  Where there is no act but relu, and no mul, and dy is bfloat16, dz is dy or 0, exactly.
+ * most), with dy in binary32 and dx in bfloat16 it is held in sixteen bits (2^-16), and with dx in binary32 in all its 24, at two
+ * and three times the products.  Where there is no act but relu, and no mul, and dy is bfloat16, dz is dy or 0, exactly.
  * The sums are binary32 over the rows in a fixed order, within (3 rows + 64) * 2^-24 * sum_r |dz W^| of the exact ones, (rows +
  * 64) for bfloat16 dy and dx; dbias sums dz itself.  Equal calls give equal bits.
  */
@@ -434,9 +434,9 @@ typedef struct {
     uint64_t ld_dy, ld_pre, ld_mul, ld_dmul, ld_dx;
 } bof4_layer_gradient;
 /* ws_dev: bof4_gemm_linear_backward_workspace_bytes(rows, cols, n_tokens) bytes (256-byte aligned), which never falls as
- * n_tokens rises: dz (in several terms as many tokens of it at a time as 4 GiB hold), partial sums, and the decoded matrix in slabs of up to
- * 256 MiB; calls that may
- * run at the same time need one each.  Limits: rows <= 2^18, cols <= 32768 and a multiple of 32, n_tokens <= 65536.  Only enqueues. */
+ * n_tokens rises and holds for any types: dz (where it takes more than bfloat16 as many tokens at a time as 4 GiB hold), partial
+ * sums, and the decoded matrix in slabs of up to 256 MiB; calls that may run at the same time need one each.  Limits: rows <=
+ * 2^18, cols <= 32768 and a multiple of 32, n_tokens <= 65536.  Only enqueues. */
 int bof4_gemm_linear_backward(const void* packed_dev, uint64_t rows, uint64_t cols, const double* cb_host, const void* table_dev,
                               uint64_t n_outliers, uint32_t n_tokens, const bof4_layer_gradient* gradient, void* ws_dev,
                               size_t ws_bytes, void* stream);

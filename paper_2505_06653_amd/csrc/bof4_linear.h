@@ -37,8 +37,8 @@ inline uint32_t linear_dz_terms(uint32_t act, bool dy_bf16, bool mul, bool mul_b
     return wanted < exact ? wanted : exact;
 }
 
-// dz in the products' order (gemm_pack_x_kernel's, rows in the place of columns, a chunk's terms behind each other): a workgroup takes a chunk of 64 rows and
-// `tiles_per_range` tiles of 32 tokens, eight threads per token, which read 128 consecutive bytes and write 16-byte words of
+// dz in the products' order (gemm_pack_x_kernel's, rows in the place of columns, a chunk's terms behind each other): a workgroup
+// takes a chunk of 64 rows and `tiles_per_range` tiles of 32 tokens, eight threads per token, which read 128 consecutive bytes and write 16-byte words of
 // which eight neighbouring tokens make up 128.  Bound by memory: 2000 tokens x 11008 rows with factor, activation and dmul, 220
 // MB, 44 us (5.0 TB/s; with 8-byte accesses 55).
 constexpr uint32_t LINEAR_MOST_RANGES = 64;  // parts of dbias at most
