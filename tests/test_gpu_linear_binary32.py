@@ -136,3 +136,43 @@ def test_tokens_in_several_passes():
     assert bool(((dy[picked].double() - g * a).abs() <= (32 * U * (1 + z.abs()) + 2 * U * a.abs()) * g.abs() + 1.01 * half_step(g * a, F32)).all())
     # slopes are below 1.2 and off by 32 U (1 + |z|); 5500 binary32 additions in chains of 1 + 32 (and binary64)
     assert bool(((dbias.double() - total).abs() <= (32 + 1.2 * 64 + 2) * U * total_abs).all())
+
+
+@pytest.mark.parametrize("rows,cols,n_tokens", [(1001, 96, 9), (100, 2080, 33), (520, 512, 300), (4111, 160, 2000)])
+@pytest.mark.parametrize("first,extra", [(0, 0), (1, 2), (4, 4)])
+def test_rows_of_any_stride_over_its_own_inputs_and_nothing_else_is_written(rows, cols, n_tokens, first, extra):
+    m = Matrix(rows, cols, 0.01)
+
+    def inside(width, dtype, seed, fill=None):
+        whole = randn((n_tokens + 2, first + width + extra), seed, dtype)
+        if fill is not None:
+            whole.fill_(fill)
+        return whole, whole[1:-1, first:first + width]
+
+    (_, dy), (_, pre), (_, mul) = inside(rows, F32, 1), inside(rows, BF16, 2), inside(rows, F32, 3)
+    dmul = torch.empty((n_tokens, rows), device=DEV)
+    want = m.backward(dy.contiguous(), act="silu", pre=pre.contiguous(), mul=mul.contiguous(), dmul=dmul, out_dtype=F32)
+    whole, dx = inside(cols, F32, 4, 7.0)
+    m.backward(dy, act="silu", pre=pre, mul=mul, out=dx)
+    assert torch.equal(dx, want)
+    whole[1:-1, first:first + cols] = 7.0
+    assert bool((whole == 7.0).all())
+    for over in ("dy", "mul"):
+        t = {"dy": dy.clone(), "mul": mul.clone()}
+        assert torch.equal(m.backward(t["dy"], act="silu", pre=pre, mul=t["mul"], dmul=t[over], out_dtype=F32), want)
+        assert torch.equal(t[over], dmul)
+
+
+def test_calls_with_other_types_side_by_side():
+    """One, two and three terms at the same time on streams of their own: what each gives alone."""
+    m, n = Matrix(4111, 2080, 0.01), 300
+    dys = [randn((n, 4111), 1, BF16), randn((n, 4111), 2, F32), randn((n, 4111), 3, F32)]
+    outs = [BF16, BF16, F32]
+    want = [m.backward(dy, out_dtype=out) for dy, out in zip(dys, outs)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in outs]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[m.backward(dy, out_dtype=out, stream=s) for dy, out, s in zip(dys, outs, streams)] for _ in range(5)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for one in got for a, b in zip(one, want))
